@@ -248,6 +248,76 @@ sra_status sra_schedule_export(const sra_problem* p, int which, int32_t* items,
 sra_status sra_launch_export(const sra_problem* p, int which, int32_t* items, int64_t items_capacity,
                              int32_t* spans, int64_t spans_capacity, int64_t* n_items, int64_t* n_spans);
 
+/* ---- language-model attention: packed prompts, and serving over a paged cache -------------
+ *
+ * The audio engine (§2.3) is a language model over discrete audio tokens. Its attention is causal, several query
+ * heads may share a K/V head, and it serves from a cache. Conventions as above, with these differences:
+ *   Tensors   q, o, do, dq are [tokens, num_heads, head_dim], k, v, dk, dv [keys, num_kv_heads, head_dim], bf16;
+ *             lse fp32 [num_heads, tokens]. num_heads = G num_kv_heads, query head h reads K/V head h / G. Inputs
+ *             q, k and v have a token stride of their own each (0 selects the dense one; q, k and v may be views
+ *             of one buffer); o, do and the gradients are dense.
+ *   Errors    as above. Device-resident sizes (sra_tree_attention, sra_cache_append) cannot be refused on the
+ *             host: what a call does for bad ones is stated there, and no such value makes it read or write
+ *             outside the tensors it was given.
+ *   Rows that see no key have o = 0, lse = -inf and no part in any gradient. So have rows whose scores are all
+ *             -inf. An infinity or NaN in v reaches, as in a product with zeros, also rows of its sequence that
+ *             do not see the key, never another sequence's.                                                  */
+
+/* Lengths of packed sequences (host memory, read by sra_causal_plan_create only). */
+typedef struct sra_causal_problem {
+  int32_t batch;             /* sequences, >= 1                                              */
+  int32_t num_heads;         /* a multiple of num_kv_heads                                   */
+  int32_t num_kv_heads;      /* >= 1                                                         */
+  int32_t head_dim;          /* 64 or 128                                                    */
+  const int32_t* q_lens;     /* [batch] query tokens, >= 0                                   */
+  const int32_t* k_lens;     /* [batch] keys, >= 0; NULL = q_lens                            */
+} sra_causal_problem;
+
+/* The tile schedule of causal attention for one set of lengths: made once, used for every layer and
+ * call with these lengths, from any thread (immutable). It holds host memory only; its tables go into
+ * a device buffer of the caller's. */
+typedef struct sra_causal_plan sra_causal_plan;
+
+/* Plans causal attention (§2.3) of packed sequences: token i of a sequence with nq tokens and nk keys sees the keys
+ * j <= i + nk - nq, so the last token sees the last key (nk > nq: the sequence continues earlier keys; with
+ * nq > nk the first nq - nk tokens see nothing). backward != 0 plans the gradients too.
+ * Host only. num_heads * tokens and num_kv_heads * keys <= 2^31 - 1 (beyond: SRA_ERR_UNSUPPORTED). */
+sra_status sra_causal_plan_create(const sra_causal_problem* p, int backward, sra_causal_plan** plan);
+
+/* Library infrastructure: frees a plan (NULL is allowed). Calls that were enqueued with it do not need it any more, only
+ * the device copy of its tables. */
+sra_status sra_causal_plan_destroy(sra_causal_plan* plan);
+
+/* Library infrastructure: bytes of the plan's tables and of the workspaces of sra_causal_forward and
+ * sra_causal_backward (0: none is needed). Any pointer may be NULL. */
+sra_status sra_causal_plan_sizes(const sra_causal_plan* plan, size_t* table_bytes, size_t* forward_workspace,
+                                 size_t* backward_workspace);
+
+/* Library infrastructure: writes the plan's tables to host memory, for the caller to copy to the device. */
+sra_status sra_causal_plan_tables(const sra_causal_plan* plan, void* host, size_t bytes);
+
+/* Host-only inspection hook: what the launches of `which` (SRA_SCHED_*) cover of the rule of
+ * sra_causal_plan_create (§2.3), for query head `head` of sequence `sequence`: out[i * nk + j] = how many items and
+ * pieces compute the pair (token i, key j) without masking it, so a correct plan gives the 0/1 mask. */
+sra_status sra_causal_plan_mask(const sra_causal_plan* plan, int which, int32_t sequence, int32_t head, uint8_t* out);
+
+/* Causal attention of packed prompts (§2.3), forward: o and lse of every query row.
+ * tables: device copy of the plan's tables, 16-byte aligned. softmax_scale <= 0 selects 1/sqrt(head_dim).
+ * Strides in elements, multiples of 8. workspace: as sra_causal_plan_sizes says, 256-byte aligned.
+ * Deterministic; enqueues kernels only, so it can be captured into a graph. */
+sra_status sra_causal_forward(const sra_causal_plan* plan, const void* tables, const void* q, const void* k,
+                              const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride, void* o,
+                              float* lse, float softmax_scale, void* workspace, size_t workspace_bytes,
+                              void* stream);
+
+/* Gradients of sra_causal_forward (§2.3; the gradient of masked softmax attention), given its o and lse and the
+ * upstream gradient dout (dense): dq, dk, dv are overwritten; dk and dv hold the sums over the query heads
+ * that share a K/V head. The plan must have been made with backward != 0. Deterministic, no atomics. */
+sra_status sra_causal_backward(const sra_causal_plan* plan, const void* tables, const void* q, const void* k,
+                               const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                               const void* o, const float* lse, const void* dout, void* dq, void* dk, void* dv,
+                               float softmax_scale, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- per-kernel timing (tracing hook; library infrastructure, no passage of the paper) --- */
 
 /* Kernels of the library, for sra_kernel_timing. */
@@ -260,7 +330,12 @@ enum {
   SRA_KERNEL_FILL = 4,      /* rows of invalid reference frames          */
   SRA_KERNEL_GATHER = 5,    /* reference rows into the compacted stream  */
   SRA_KERNEL_SCATTER = 6,   /* compacted rows back to the reference rows */
-  SRA_KERNEL_COUNT = 7
+  SRA_KERNEL_CAUSAL_FORWARD = 7,  /* sra_causal_forward                  */
+  SRA_KERNEL_CAUSAL_DELTA = 8,    /* sra_causal_backward: D              */
+  SRA_KERNEL_CAUSAL_GRAD = 9,     /* sra_causal_backward: dQ, dK and dV  */
+  SRA_KERNEL_TREE = 10,           /* sra_tree_attention                  */
+  SRA_KERNEL_APPEND = 11,         /* sra_cache_append                    */
+  SRA_KERNEL_COUNT = 12
 };
 
 /* enable != 0: from now on every kernel launch is bracketed by two hipEvents recorded on the

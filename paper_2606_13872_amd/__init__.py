@@ -19,3 +19,4 @@ from .sra import (  # noqa: F401
     schedule_mask,
     useful_flops,
 )
+from .causal import CausalPlan, causal_backward, causal_forward  # noqa: F401

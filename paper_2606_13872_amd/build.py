@@ -19,7 +19,9 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libsra.so")
 
 SOURCES = ["schedule.cpp", "sra_api.cpp", "sra_fwd.hip", "sra_fwd32.hip", "sra_bwd.hip", "sra_grad.hip",
-           "sra_compact.hip", "sra_noalloc.hip"]
+           "sra_compact.hip", "sra_noalloc.hip", "causal_plan.cpp", "sra_text_api.cpp", "sra_causal_fwd.hip",
+           "sra_causal_bwd.hip"]
+HIP_HOST = ("sra_api.cpp", "sra_text_api.cpp")  # host code that includes the HIP runtime's headers
 
 COMMON = [
     "-O3", "-std=c++17", "-fPIC", "-Wall",
@@ -28,10 +30,10 @@ COMMON = [
 # Device code only for gfx950. Packed-FP32 instructions are disabled in device code.
 HIP_FLAGS = ["-x", "hip", "--offload-arch=gfx950", "-Xclang", "-target-feature",
              "-Xclang", "-packed-fp32-ops"]
-# The dK/dV and dQ kernels (sra_grad.hip) select their compiler-visible MFMAs in VGPR form: their AGPRs hold
+# The dK/dV and dQ kernels (sra_grad.hip, sra_causal_bwd.hip) select their compiler-visible MFMAs in VGPR form: their AGPRs hold
 # the gradient sums (written by inline-assembly MFMAs), and S/dP must stay in VGPRs next to them.
 _VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
-EXTRA_FLAGS = {"sra_grad.hip": _VGPR_FORM}
+EXTRA_FLAGS = {"sra_grad.hip": _VGPR_FORM, "sra_causal_bwd.hip": _VGPR_FORM}
 COMPILE_TIMEOUT_S = 900
 
 
@@ -47,8 +49,8 @@ def _compile(src: str) -> str:
     path = os.path.join(CSRC, src)
     if src.endswith(".hip"):
         cmd = [hipcc(), *HIP_FLAGS, *EXTRA_FLAGS.get(src, []), *COMMON, "-c", path, "-o", obj]
-    else:  # host-only C++ (the scheduler includes no HIP header)
-        cmd = [hipcc(), *COMMON, "-c", path, "-o", obj] if src == "sra_api.cpp" else \
+    else:  # host-only C++ (the schedulers include no HIP header)
+        cmd = [hipcc(), *COMMON, "-c", path, "-o", obj] if src in HIP_HOST else \
               ["g++", *COMMON, "-c", path, "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True, timeout=COMPILE_TIMEOUT_S)
     if r.returncode != 0:
@@ -81,7 +83,7 @@ def build(verbose: bool = False) -> str:
 #   UBSAN_OPTIONS=halt_on_error=1:print_stacktrace=1 python -m pytest tests/test_schedule.py tests/test_abi.py
 SAN_DIR = os.path.join(BUILD, "sanitize")
 SAN_LIB = os.path.join(SAN_DIR, "libsra_host.so")
-SAN_SOURCES = ["schedule.cpp", "sra_api.cpp", "sra_host_stubs.cpp"]
+SAN_SOURCES = ["schedule.cpp", "sra_api.cpp", "causal_plan.cpp", "sra_text_api.cpp", "sra_host_stubs.cpp"]
 SAN_FLAGS = ["-fsanitize=address,undefined", "-fno-sanitize-recover=undefined", "-fno-omit-frame-pointer", "-g",
              "-O1"]
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")

@@ -1,0 +1,216 @@
+"""Causal attention of packed prompts with grouped heads (include/sra.h, sra_causal_*): argument marshalling.
+
+    plan = CausalPlan(q_lens, heads, kv_heads, head_dim)       # once per set of lengths
+    o, lse = causal_forward(q, k, v, plan)                     # every layer
+    g = causal_backward(q, k, v, o, lse, do, plan)             # g["dq"], g["dk"], g["dv"]
+"""
+from __future__ import annotations
+
+import ctypes
+import weakref
+from typing import Dict, Optional, Sequence
+
+import numpy as np
+
+from . import sra as _s
+
+_handles_declared = False
+
+
+class _CausalProblem(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("num_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("q_lens", ctypes.c_void_p), ("k_lens", ctypes.c_void_p)]
+
+
+def _lib():
+    global _handles_declared
+    L = _s.lib()
+    if not _handles_declared:
+        vp, i32, i64, sz, f = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
+        psz = ctypes.POINTER(sz)
+        for name, args in {
+            "sra_causal_plan_create": [ctypes.POINTER(_CausalProblem), ctypes.c_int, ctypes.POINTER(vp)],
+            "sra_causal_plan_destroy": [vp],
+            "sra_causal_plan_sizes": [vp, psz, psz, psz],
+            "sra_causal_plan_tables": [vp, vp, sz],
+            "sra_causal_plan_mask": [vp, ctypes.c_int, i32, i32, vp],
+            "sra_causal_forward": [vp] * 5 + [i64] * 3 + [vp, vp, f, vp, sz, vp],
+            "sra_causal_backward": [vp] * 5 + [i64] * 3 + [vp] * 6 + [f, vp, sz, vp],
+        }.items():
+            fn = getattr(L, name)
+            fn.argtypes = args
+            fn.restype = ctypes.c_int
+        _handles_declared = True
+    return L
+
+
+def _lens(x, name) -> np.ndarray:
+    a = np.asarray(x.detach().cpu() if hasattr(x, "detach") else x)
+    if a.ndim != 1 or a.size == 0 or a.dtype.kind not in "iu":
+        raise _s._bad(f"{name} must be a non-empty sequence of integers")
+    if a.min() < 0 or a.max() > 2**31 - 1:
+        raise _s._bad(f"{name}: lengths must be between 0 and 2^31 - 1")
+    return np.ascontiguousarray(a.astype(np.int32))
+
+
+class CausalPlan:
+    """The tile schedule of causal attention for one set of lengths, with its tables on `device` (default: the
+    current GPU; without a GPU only the host hooks work). Made once, used by every layer and call with these lengths.
+
+    q_lens: tokens of each packed sequence. k_lens: its keys, where they differ (the sequence continues earlier
+    keys: token i of nq sees the keys j <= i + nk - nq). backward=False plans the forward alone.
+    """
+
+    def __init__(self, q_lens: Sequence[int], heads: int, kv_heads: int, head_dim: int,
+                 k_lens: Optional[Sequence[int]] = None, backward: bool = True, device=None):
+        L = _lib()
+        self.q_lens = _lens(q_lens, "q_lens")
+        self.k_lens = self.q_lens if k_lens is None else _lens(k_lens, "k_lens")
+        if self.k_lens.shape != self.q_lens.shape:
+            raise _s._bad("q_lens and k_lens must have one length per sequence each")
+        self.heads, self.kv_heads, self.head_dim, self.backward = int(heads), int(kv_heads), int(head_dim), bool(backward)
+        p = _CausalProblem(len(self.q_lens), self.heads, self.kv_heads, self.head_dim, self.q_lens.ctypes.data,
+                           self.k_lens.ctypes.data)
+        h = ctypes.c_void_p()
+        _s._check(L.sra_causal_plan_create(ctypes.byref(p), 1 if backward else 0, ctypes.byref(h)))
+        self._handle = h
+        self._finalizer = weakref.finalize(self, L.sra_causal_plan_destroy, h)
+        t, f, b = ctypes.c_size_t(), ctypes.c_size_t(), ctypes.c_size_t()
+        _s._check(L.sra_causal_plan_sizes(h, ctypes.byref(t), ctypes.byref(f), ctypes.byref(b)))
+        self._table_bytes, self.forward_workspace, self.backward_workspace = t.value, f.value, b.value
+        self.n_q, self.n_k = int(self.q_lens.sum(dtype=np.int64)), int(self.k_lens.sum(dtype=np.int64))
+        self._tables = {}
+        torch = _s._tm()
+        if device is not None or torch.cuda.is_available():
+            dev = torch.device("cuda" if device is None else device)
+            if dev.type != "cuda":
+                raise _s._bad(f"a plan's tables must be on a GPU (HIP device), got {dev}")
+            self._upload(torch.cuda.current_device() if dev.index is None else dev.index)
+
+    def _upload(self, index: int):
+        """The tables on GPU `index` (its address and the stream that they were copied on)."""
+        torch = _s._tm()
+        host = np.zeros(max(1, self._table_bytes), dtype=np.uint8)
+        _s._check(_lib().sra_causal_plan_tables(self._handle, host.ctypes.data, self._table_bytes))
+        with torch.cuda.device(index):
+            t = torch.from_numpy(host).to(torch.device("cuda", index))
+            torch.cuda.current_stream().synchronize()  # any stream may read them from now on
+            self._tables[index] = (t, torch.cuda.current_stream().cuda_stream)
+        return self._tables[index]
+
+    def _device_tables(self, dev, stream):
+        """Address of the tables on `dev`, kept for the work that is enqueued on `stream` now."""
+        t, home = self._tables.get(dev.index) or self._upload(dev.index)
+        if stream.value != home and (stream.value or home):
+            t.record_stream(_s._tm().cuda.current_stream(dev))
+        return ctypes.c_void_p(t.data_ptr())
+
+    def mask(self, which: int, sequence: int, head: int) -> np.ndarray:
+        """sra_causal_plan_mask: how often launch `which` (SCHED_*) computes each (token, key) pair."""
+        ok = 0 <= sequence < len(self.q_lens)
+        out = np.zeros((self.q_lens[sequence], self.k_lens[sequence]) if ok else (1, 1), dtype=np.uint8)
+        buf = out if out.size else np.zeros(1, dtype=np.uint8)
+        _s._check(_lib().sra_causal_plan_mask(self._handle, which, sequence, head, buf.ctypes.data))
+        return out
+
+
+def _stride(t, name):
+    """Token stride of an input [tokens, heads, head_dim] with contiguous heads (0: it has at most one token)."""
+    if t.shape[0] <= 1:
+        return 0
+    s = int(t.stride(0))
+    if s < t.shape[1] * t.shape[2]:
+        raise _s._bad(f"{name}: tokens overlap (stride {s})")
+    return s
+
+
+def _qkv(q, k, v, plan):
+    torch = _s._tm()
+    if not isinstance(plan, CausalPlan):
+        raise _s._bad("plan must be a CausalPlan")
+    bf = torch.bfloat16
+    _s._expect(q, "q", (plan.n_q, plan.heads, plan.head_dim), bf, False)
+    _s._expect(k, "k", (plan.n_k, plan.kv_heads, plan.head_dim), bf, False)
+    _s._expect(v, "v", (plan.n_k, plan.kv_heads, plan.head_dim), bf, False)
+    return _stride(q, "q"), _stride(k, "k"), _stride(v, "v")
+
+
+def _no_alias(out, named):
+    """Output buffers must not share memory with inputs or each other (they are written while inputs are read)."""
+    spans = []
+    for name, t in named:
+        if t is None or t.numel() == 0:
+            continue
+        a = t.data_ptr()
+        b = a + t.element_size() * (sum((n - 1) * s for n, s in zip(t.shape, t.stride())) + 1)
+        for other, c, d, w in spans:
+            if a < d and c < b and (w or name in out):
+                raise _s._bad(f"output {name if name in out else other} overlaps {other if name in out else name}")
+        spans.append((name, a, b, name in out))
+
+
+def _call(dev, fn):
+    """fn(stream) with `dev` as the current device."""
+    torch = _s._tm()
+    if torch.cuda.current_device() == dev.index:
+        return fn(_s._stream_ptr(dev))
+    with torch.cuda.device(dev):
+        return fn(_s._stream_ptr(dev))
+
+
+def causal_forward(q, k, v, plan: CausalPlan, scale: Optional[float] = None, out: Optional[Dict] = None):
+    """Causal attention of packed prompts. Returns (o, lse).
+
+    q: bf16 [tokens, heads, head_dim], k, v: bf16 [keys, kv_heads, head_dim], heads contiguous, a token stride each
+    (views of one packed buffer work); query head h reads K/V head h // (heads // kv_heads). o: bf16 like q, dense;
+    lse: fp32 [heads, tokens], natural log. Rows that see no key have o = 0 and lse = -inf. `out` may hold caller
+    buffers o, lse (dense) and workspace (uint8), which must not overlap the inputs. A wrong dtype, shape, layout or
+    device raises SRAError (SRA_ERR_INVALID_ARGUMENT) before anything reaches the library.
+    """
+    torch = _s._tm()
+    qs, ks, vs = _qkv(q, k, v, plan)
+    o_shape, lse_shape = (plan.n_q, plan.heads, plan.head_dim), (plan.heads, plan.n_q)
+    _s._precheck_outs(out, [("o", o_shape, torch.bfloat16), ("lse", lse_shape, torch.float32)])
+    dev = q.device
+    _s._same_device((("q", q), ("k", k), ("v", v)), dev)
+    out = out or {}
+    o = _s._out(out, "o", o_shape, torch.bfloat16, dev)
+    lse = _s._out(out, "lse", lse_shape, torch.float32, dev)
+    ws = _s._workspace(out, plan.forward_workspace, dev)
+    if out:
+        _no_alias(out, (("q", q), ("k", k), ("v", v), ("o", o), ("lse", lse), ("workspace", ws)))
+    _s._check(_call(dev, lambda s: _lib().sra_causal_forward(
+        plan._handle, plan._device_tables(dev, s), _s._ptr(q), _s._ptr(k), _s._ptr(v), qs, ks, vs, _s._ptr(o),
+        _s._ptr(lse), 0.0 if scale is None else float(scale), _s._ptr(ws), ws.numel(), s)))
+    return o, lse
+
+
+def causal_backward(q, k, v, o, lse, do, plan: CausalPlan, scale: Optional[float] = None, out: Optional[Dict] = None):
+    """Gradients of causal_forward. Returns dict dq, dk, dv (bf16, dense, overwritten).
+
+    o and lse as causal_forward wrote them, do: bf16 like o, dense. dk and dv are summed over the query heads that
+    share a K/V head. `out` may hold caller buffers dq, dk, dv (dense) and workspace (uint8).
+    """
+    torch = _s._tm()
+    qs, ks, vs = _qkv(q, k, v, plan)
+    if not plan.backward:
+        raise _s._bad("the plan was made with backward=False")
+    bf = torch.bfloat16
+    q_shape, k_shape = (plan.n_q, plan.heads, plan.head_dim), (plan.n_k, plan.kv_heads, plan.head_dim)
+    _s._expect(o, "o", q_shape, bf, True)
+    _s._expect(do, "do", q_shape, bf, True)
+    _s._expect(lse, "lse", (plan.heads, plan.n_q), torch.float32, True)
+    _s._precheck_outs(out, [("dq", q_shape, bf), ("dk", k_shape, bf), ("dv", k_shape, bf)])
+    dev = q.device
+    _s._same_device((("q", q), ("k", k), ("v", v), ("o", o), ("lse", lse), ("do", do)), dev)
+    out = out or {}
+    g = {"dq": _s._out(out, "dq", q_shape, bf, dev), "dk": _s._out(out, "dk", k_shape, bf, dev),
+         "dv": _s._out(out, "dv", k_shape, bf, dev)}
+    ws = _s._workspace(out, plan.backward_workspace, dev)
+    if out:
+        _no_alias(out, (("q", q), ("k", k), ("v", v), ("o", o), ("lse", lse), ("do", do), *g.items(), ("workspace", ws)))
+    _s._check(_call(dev, lambda s: _lib().sra_causal_backward(
+        plan._handle, plan._device_tables(dev, s), _s._ptr(q), _s._ptr(k), _s._ptr(v), qs, ks, vs, _s._ptr(o),
+        _s._ptr(lse), _s._ptr(do), _s._ptr(g["dq"]), _s._ptr(g["dk"]), _s._ptr(g["dv"]),
+        0.0 if scale is None else float(scale), _s._ptr(ws), ws.numel(), s)))
+    return g

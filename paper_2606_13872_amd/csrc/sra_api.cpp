@@ -555,6 +555,10 @@ sra_status forward_call(const sra_problem* p, const void* q_gen, const void* k_g
 
 sra_status set_error(sra_status s, const char* msg) { return fail(s, msg); }
 
+hipError_t timed_launch(int kernel, hipStream_t stream, const std::function<hipError_t()>& launch) {
+  return timed(kernel, stream, launch);
+}
+
 }  // namespace sra
 
 extern "C" {

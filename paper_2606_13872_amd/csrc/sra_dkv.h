@@ -52,9 +52,10 @@ struct DkvAddr {
 // registers = query rows, so P and dS are directly the B fragments of the products they enter.
 // Each MFMA is followed by its share of the vector work (a 16x16x32 MFMA hides about 8 cycles of
 // it) and a scheduling barrier; LDS fragments are read one group of four MFMAs ahead. Rows
-// outside the span have LSE = +inf, so P = 0. kRange: the lane's key of block kb takes part only
-// if bit kb of kv is set. hook(u) runs behind MFMA group u of the half's D / 4.
-template <int D, bool kRange, class Hook>
+// outside the span have LSE = +inf, so P = 0. kMask 1: the lane's key of block kb takes part only
+// if bit kb of kv is set; 2: query i of block qb sees it only if kv + 16 (qb - kb) + i >= 0 (causal
+// attention). hook(u) runs behind MFMA group u of the half's D / 4.
+template <int D, int kMask, class Hook>
 __device__ __forceinline__ void dkv_half(DkvState<D>& st, const DkvAddr& ad, uint32_t qt, uint32_t dt, uint32_t stat,
                                          uint32_t qtp, float sl2, int kv, Hook hook) {
   constexpr int NC = D / 32, NG = D / 16;  // NG groups of four MFMAs per product
@@ -89,7 +90,8 @@ __device__ __forceinline__ void dkv_half(DkvState<D>& st, const DkvAddr& ad, uin
       s[b][i] = fmaf(s[b][i], sl2, -l4[qb][i]);
     } else {
       float y = fast_exp2(s[b][i]);
-      if constexpr (kRange) y = (kv >> kb) & 1 ? y : 0.f;
+      if constexpr (kMask == 1) y = (kv >> kb) & 1 ? y : 0.f;
+      if constexpr (kMask == 2) y = kv + 16 * (qb - kb) + i >= 0 ? y : 0.f;
       s[b][i] = y;
       if (i & 1) {
         pb[kb][4 * qb + i - 1] = (__bf16)s[b][i - 1];

@@ -2,6 +2,7 @@
 // `build.py --sanitize`, never shipped): the scheduler and the C ABI are compiled with
 // AddressSanitizer and UndefinedBehaviorSanitizer for the CPU, and every launch reports
 // hipErrorNotSupported, so a call that gets past validation fails with SRA_ERR_HIP.
+#include "sra_causal_kernels.h"
 #include "sra_kernels.h"
 
 namespace sra {
@@ -18,5 +19,14 @@ hipError_t launch_grad_combine(const BwdArgs&, const CombineItem*, int, int, int
 hipError_t launch_fill(const FillArgs&, hipStream_t) { return hipErrorNotSupported; }
 hipError_t launch_gather(const GatherArgs&, hipStream_t) { return hipErrorNotSupported; }
 hipError_t launch_scatter(const ScatterArgs&, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_causal_forward(const CausalArgs&, int, int, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_causal_forward_combine(const CausalArgs&, const CausalItem*, int, int, hipStream_t) {
+  return hipErrorNotSupported;
+}
+hipError_t launch_causal_delta(const CausalDeltaArgs&, int, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_causal_grad(const CausalArgs&, int, int, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_causal_grad_combine(const CausalArgs&, const CausalItem*, int, int, hipStream_t) {
+  return hipErrorNotSupported;
+}
 
 }  // namespace sra

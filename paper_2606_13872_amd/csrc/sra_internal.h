@@ -1,6 +1,9 @@
 // Library-internal entry points shared by the C ABI translation units.
 #pragma once
+#include <hip/hip_runtime.h>
 #include <stddef.h>
+
+#include <functional>
 
 #include "sra.h"
 
@@ -29,5 +32,8 @@ sra_status forward_call(const sra_problem* p, const void* q_gen, const void* k_g
 
 // Sets the thread's last-error message and returns `s`.
 sra_status set_error(sra_status s, const char* msg);
+
+// Runs `launch` (kernel launches on `stream`), timed as kernel `kernel` where timing is on.
+hipError_t timed_launch(int kernel, hipStream_t stream, const std::function<hipError_t()>& launch);
 
 }  // namespace sra

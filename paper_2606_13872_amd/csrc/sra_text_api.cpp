@@ -1,0 +1,293 @@
+// C ABI of causal attention over packed prompts (include/sra.h): validation, plans and launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstring>
+#include <memory>
+#include <new>
+#include <string>
+
+#include "sra.h"
+#include "sra_causal_kernels.h"
+#include "sra_internal.h"
+
+struct sra_causal_plan {
+  sra::CausalTables t;
+  // tables in the device buffer: fwd | fwd_combine | grad | grad_combine
+  size_t offset[4] = {0, 0, 0, 0};
+  size_t table_bytes = 0, forward_workspace = 0, backward_workspace = 0, stat_bytes = 0, part_q_bytes = 0;
+};
+
+namespace {
+
+using namespace sra;
+
+constexpr size_t kAlign = 256;
+constexpr int64_t kMaxInt = 2147483647;
+constexpr int64_t kMaxStride = kMaxInt / 64;  // offsets inside a tile are 32-bit
+
+size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+sra_status fail(sra_status s, const std::string& msg) { return set_error(s, msg.c_str()); }
+sra_status hip_fail(hipError_t e, const char* what) { return fail(SRA_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e)); }
+bool misaligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; }
+
+const std::vector<CausalItem>* lists(const CausalTables& t, int i) {
+  const std::vector<CausalItem>* l[4] = {&t.fwd, &t.fwd_combine, &t.grad, &t.grad_combine};
+  return l[i];
+}
+
+// Heads and head_dim of every call here.
+sra_status check_heads(int32_t heads, int32_t kv_heads, int32_t head_dim) {
+  if (heads < 1 || kv_heads < 1 || heads % kv_heads)
+    return fail(SRA_ERR_INVALID_ARGUMENT, "num_heads must be a positive multiple of num_kv_heads");
+  if (head_dim < 1) return fail(SRA_ERR_INVALID_ARGUMENT, "head_dim must be positive");
+  if (head_dim != 64 && head_dim != 128) return fail(SRA_ERR_UNSUPPORTED, "head_dim must be 64 or 128");
+  return SRA_OK;
+}
+
+// A token stride: 0 selects the dense one.
+sra_status check_stride(int64_t* stride, int32_t heads, int32_t head_dim, const char* name) {
+  const int64_t dense = int64_t(heads) * head_dim;
+  if (*stride == 0) *stride = dense;
+  if (*stride < dense || *stride % 8)
+    return fail(SRA_ERR_INVALID_ARGUMENT, std::string(name) + " stride must be a multiple of 8 and at least heads * head_dim");
+  if (*stride > kMaxStride) return fail(SRA_ERR_UNSUPPORTED, std::string(name) + " stride is too large");
+  return SRA_OK;
+}
+
+sra_status check_pointers(std::initializer_list<const void*> ps) {
+  for (const void* p : ps) {
+    if (!p) return fail(SRA_ERR_INVALID_ARGUMENT, "a tensor pointer is NULL");
+    if (misaligned(p, 16)) return fail(SRA_ERR_INVALID_ARGUMENT, "tensor pointers must be 16-byte aligned");
+  }
+  return SRA_OK;
+}
+
+sra_status check_workspace(const void* ws, size_t bytes, size_t need) {
+  if (bytes < need) return fail(SRA_ERR_WORKSPACE_TOO_SMALL, "the call needs " + std::to_string(need) + " workspace bytes");
+  if (need && (!ws || misaligned(ws, kAlign)))
+    return fail(SRA_ERR_INVALID_ARGUMENT, "workspace must be non-NULL and 256-byte aligned");
+  return SRA_OK;
+}
+
+float scale_of(float scale, int32_t head_dim) {
+  return scale > 0 ? scale : float(1.0 / __builtin_sqrt(double(head_dim)));
+}
+
+// Checks of a causal call before anything is enqueued, and the arguments both directions share.
+sra_status causal_args(const sra_causal_plan* plan, const void* tables, const void* q, const void* k, const void* v,
+                       int64_t q_stride, int64_t k_stride, int64_t v_stride, float scale, CausalArgs* a) {
+  if (!plan) return fail(SRA_ERR_INVALID_ARGUMENT, "plan is NULL");
+  const CausalTables& t = plan->t;
+  sra_status st = check_stride(&q_stride, t.heads, t.head_dim, "q");
+  if (st == SRA_OK) st = check_stride(&k_stride, t.kv_heads, t.head_dim, "k");
+  if (st == SRA_OK) st = check_stride(&v_stride, t.kv_heads, t.head_dim, "v");
+  if (st != SRA_OK) return st;
+  if (!(scale == scale) || scale > 3.0e38f) return fail(SRA_ERR_INVALID_ARGUMENT, "softmax_scale must be finite");
+  if (t.q_rows && (st = check_pointers({q})) != SRA_OK) return st;
+  if (t.k_rows && (st = check_pointers({k, v})) != SRA_OK) return st;
+  if (plan->table_bytes && (!tables || misaligned(tables, 16)))
+    return fail(SRA_ERR_INVALID_ARGUMENT, "tables must be non-NULL and 16-byte aligned");
+  a->q = static_cast<const __bf16*>(q);
+  a->k = static_cast<const __bf16*>(k);
+  a->v = static_cast<const __bf16*>(v);
+  a->qs = q_stride;
+  a->ks = k_stride;
+  a->vs = v_stride;
+  a->q_rows = int32_t(t.q_rows);
+  a->heads = t.heads;
+  a->kv_heads = t.kv_heads;
+  a->scale = scale_of(scale, t.head_dim);
+  a->scale_log2 = float(double(a->scale) * 1.4426950408889634);
+  return SRA_OK;
+}
+
+const CausalItem* table(const sra_causal_plan* p, const void* tables, int i) {
+  return reinterpret_cast<const CausalItem*>(static_cast<const char*>(tables) + p->offset[i]);
+}
+
+}  // namespace
+
+extern "C" {
+
+sra_status sra_causal_plan_create(const sra_causal_problem* p, int backward, sra_causal_plan** plan) {
+  set_error(SRA_OK, "");
+  if (!p || !plan) return fail(SRA_ERR_INVALID_ARGUMENT, "problem or plan is NULL");
+  *plan = nullptr;
+  sra_status st = check_heads(p->num_heads, p->num_kv_heads, p->head_dim);
+  if (st != SRA_OK) return st;
+  if (p->batch < 1 || !p->q_lens) return fail(SRA_ERR_INVALID_ARGUMENT, "batch must be positive and q_lens given");
+  try {
+    std::unique_ptr<sra_causal_plan> c(new sra_causal_plan);
+    CausalTables& t = c->t;
+    t.batch = p->batch;
+    t.heads = p->num_heads;
+    t.kv_heads = p->num_kv_heads;
+    t.head_dim = p->head_dim;
+    t.backward = backward != 0;
+    const int32_t* k_lens = p->k_lens ? p->k_lens : p->q_lens;
+    for (int32_t b = 0; b < p->batch; ++b) {
+      if (p->q_lens[b] < 0 || k_lens[b] < 0) return fail(SRA_ERR_INVALID_ARGUMENT, "lengths must not be negative");
+      t.nq.push_back(p->q_lens[b]);
+      t.nk.push_back(k_lens[b]);
+      t.q_rows += p->q_lens[b];
+      t.k_rows += k_lens[b];
+    }
+    if (t.q_rows * t.heads > kMaxInt || t.k_rows * t.kv_heads > kMaxInt)
+      return fail(SRA_ERR_UNSUPPORTED, "heads * packed tokens must be below 2^31");
+    build_causal_tables(&t);
+    size_t at = 0;
+    for (int i = 0; i < 4; ++i) {
+      c->offset[i] = at;
+      at += align_up(lists(t, i)->size() * sizeof(CausalItem));
+    }
+    c->table_bytes = at;
+    c->forward_workspace = align_up(size_t(t.fwd_slots) * kCausalTile * (t.head_dim + 2) * 4);
+    if (t.backward) {
+      c->stat_bytes = align_up(size_t(t.heads) * t.q_rows * 4);
+      c->part_q_bytes = align_up(size_t(t.q_slots) * kCausalTile * t.head_dim * 4);
+      c->backward_workspace = 2 * c->stat_bytes + c->part_q_bytes +
+                              align_up(size_t(t.kv_slots) * 2 * kCausalTile * t.head_dim * 4);
+    }
+    *plan = c.release();
+  } catch (const std::bad_alloc&) {
+    return fail(SRA_ERR_INTERNAL, "out of host memory");
+  } catch (...) {
+    return fail(SRA_ERR_INTERNAL, "planning failed");
+  }
+  return SRA_OK;
+}
+
+sra_status sra_causal_plan_destroy(sra_causal_plan* plan) {
+  set_error(SRA_OK, "");
+  delete plan;
+  return SRA_OK;
+}
+
+sra_status sra_causal_plan_sizes(const sra_causal_plan* plan, size_t* table_bytes, size_t* forward_workspace,
+                                 size_t* backward_workspace) {
+  set_error(SRA_OK, "");
+  if (!plan) return fail(SRA_ERR_INVALID_ARGUMENT, "plan is NULL");
+  if (table_bytes) *table_bytes = plan->table_bytes;
+  if (forward_workspace) *forward_workspace = plan->forward_workspace;
+  if (backward_workspace) *backward_workspace = plan->backward_workspace;
+  return SRA_OK;
+}
+
+sra_status sra_causal_plan_tables(const sra_causal_plan* plan, void* host, size_t bytes) {
+  set_error(SRA_OK, "");
+  if (!plan || (!host && plan->table_bytes)) return fail(SRA_ERR_INVALID_ARGUMENT, "plan or host buffer is NULL");
+  if (bytes < plan->table_bytes) return fail(SRA_ERR_INVALID_ARGUMENT, "the host buffer is smaller than the tables");
+  if (plan->table_bytes) std::memset(host, 0, plan->table_bytes);
+  for (int i = 0; i < 4; ++i) {
+    const std::vector<CausalItem>& l = *lists(plan->t, i);
+    if (!l.empty()) std::memcpy(static_cast<char*>(host) + plan->offset[i], l.data(), l.size() * sizeof(CausalItem));
+  }
+  return SRA_OK;
+}
+
+sra_status sra_causal_plan_mask(const sra_causal_plan* plan, int which, int32_t sequence, int32_t head, uint8_t* out) {
+  set_error(SRA_OK, "");
+  if (!plan || !out) return fail(SRA_ERR_INVALID_ARGUMENT, "plan or out is NULL");
+  const CausalTables& t = plan->t;
+  if (which != SRA_SCHED_FORWARD && which != SRA_SCHED_BWD_DQ && which != SRA_SCHED_BWD_DKDV)
+    return fail(SRA_ERR_INVALID_ARGUMENT, "unknown schedule");
+  if (sequence < 0 || sequence >= t.batch || head < 0 || head >= t.heads)
+    return fail(SRA_ERR_INVALID_ARGUMENT, "sequence or head out of range");
+  if (which != SRA_SCHED_FORWARD && !t.backward) return fail(SRA_ERR_INVALID_ARGUMENT, "the plan has no backward");
+  const int32_t G = t.heads / t.kv_heads, kvh = head / G, hg = head % G, nq = t.nq[sequence], nk = t.nk[sequence];
+  const CausalKind kind = which == SRA_SCHED_FORWARD ? kForward : which == SRA_SCHED_BWD_DQ ? kDq : kDkv;
+  std::memset(out, 0, size_t(nq) * nk);
+  for (const CausalItem& it : which == SRA_SCHED_FORWARD ? t.fwd : t.grad) {
+    if (it.kind != kind || it.seq != sequence || it.kvh != kvh) continue;
+    if (kind != kDkv) {
+      for (int32_t r = it.start; r < it.start + it.len; ++r) {
+        if (r % G != hg) continue;
+        const int32_t i = r / G;
+        for (int32_t j = it.lo; j < it.hi && j <= i + nk - nq; ++j) out[size_t(i) * nk + j]++;
+      }
+    } else {
+      const CausalTiles tiles = causal_tiles(it);
+      for (int32_t x = it.lo; x < it.hi; ++x) {
+        const CausalTile c = causal_tile(tiles, G, x);
+        if (c.hg != hg) continue;
+        const int32_t first = c.tok;
+        const bool masked = first + nk - nq < it.start + it.len - 1;
+        if (masked != (x >= G * (tiles.n - tiles.d))) return fail(SRA_ERR_INTERNAL, "a tile of the wrong kind");
+        for (int32_t i = first; i < std::min(first + 64, nq); ++i)
+          for (int32_t j = it.start; j < it.start + it.len && j <= i + nk - nq; ++j) out[size_t(i) * nk + j]++;
+      }
+    }
+  }
+  return SRA_OK;
+}
+
+sra_status sra_causal_forward(const sra_causal_plan* plan, const void* tables, const void* q, const void* k,
+                              const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride, void* o,
+                              float* lse, float softmax_scale, void* workspace, size_t workspace_bytes,
+                              void* stream) {
+  set_error(SRA_OK, "");
+  CausalArgs a{};
+  sra_status st = causal_args(plan, tables, q, k, v, q_stride, k_stride, v_stride, softmax_scale, &a);
+  if (st != SRA_OK) return st;
+  const CausalTables& t = plan->t;
+  if (t.q_rows && (st = check_pointers({o, lse})) != SRA_OK) return st;
+  st = check_workspace(workspace, workspace_bytes, plan->forward_workspace);
+  if (st != SRA_OK) return st;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  a.items = table(plan, tables, 0);
+  a.o = static_cast<__bf16*>(o);
+  a.lse = lse;
+  a.part = static_cast<float*>(workspace);
+  const hipError_t e = timed_launch(SRA_KERNEL_CAUSAL_FORWARD, s, [&] {
+    const hipError_t x = launch_causal_forward(a, int(t.fwd.size()), t.head_dim, s);
+    if (x != hipSuccess) return x;
+    return launch_causal_forward_combine(a, table(plan, tables, 1), int(t.fwd_combine.size()), t.head_dim, s);
+  });
+  return e == hipSuccess ? SRA_OK : hip_fail(e, "causal forward launch");
+}
+
+sra_status sra_causal_backward(const sra_causal_plan* plan, const void* tables, const void* q, const void* k,
+                               const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                               const void* o, const float* lse, const void* dout, void* dq, void* dk, void* dv,
+                               float softmax_scale, void* workspace, size_t workspace_bytes, void* stream) {
+  set_error(SRA_OK, "");
+  CausalArgs a{};
+  sra_status st = causal_args(plan, tables, q, k, v, q_stride, k_stride, v_stride, softmax_scale, &a);
+  if (st != SRA_OK) return st;
+  const CausalTables& t = plan->t;
+  if (!t.backward) return fail(SRA_ERR_INVALID_ARGUMENT, "the plan was made without the backward");
+  if (t.q_rows && (st = check_pointers({o, lse, dout, dq})) != SRA_OK) return st;
+  if (t.k_rows && (st = check_pointers({dk, dv})) != SRA_OK) return st;
+  st = check_workspace(workspace, workspace_bytes, plan->backward_workspace);
+  if (st != SRA_OK) return st;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  char* ws = static_cast<char*>(workspace);
+  CausalDeltaArgs d{};
+  d.o = static_cast<const __bf16*>(o);
+  d.dout = static_cast<const __bf16*>(dout);
+  d.lse = lse;
+  d.lse2 = reinterpret_cast<float*>(ws);
+  d.ndelta = reinterpret_cast<float*>(ws + plan->stat_bytes);
+  d.q_rows = a.q_rows;
+  d.heads = a.heads;
+  hipError_t e = timed_launch(SRA_KERNEL_CAUSAL_DELTA, s, [&] { return launch_causal_delta(d, t.head_dim, s); });
+  if (e != hipSuccess) return hip_fail(e, "causal delta launch");
+  a.items = table(plan, tables, 2);
+  a.dout = d.dout;
+  a.lse2 = d.lse2;
+  a.ndelta = d.ndelta;
+  a.dq = static_cast<__bf16*>(dq);
+  a.dk = static_cast<__bf16*>(dk);
+  a.dv = static_cast<__bf16*>(dv);
+  a.part_q = reinterpret_cast<float*>(ws + 2 * plan->stat_bytes);
+  a.part_kv = reinterpret_cast<float*>(ws + 2 * plan->stat_bytes + plan->part_q_bytes);
+  e = timed_launch(SRA_KERNEL_CAUSAL_GRAD, s, [&] {
+    const hipError_t x = launch_causal_grad(a, int(t.grad.size()), t.head_dim, s);
+    if (x != hipSuccess) return x;
+    return launch_causal_grad_combine(a, table(plan, tables, 3), int(t.grad_combine.size()), t.head_dim, s);
+  });
+  return e == hipSuccess ? SRA_OK : hip_fail(e, "causal gradient launch");
+}
+
+}  // extern "C"

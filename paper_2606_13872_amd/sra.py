@@ -302,7 +302,8 @@ def release_caches() -> None:
     _check(lib().sra_release_caches())
 
 
-KERNELS = {"forward": 0, "delta": 1, "dkdv": 2, "dq": 3, "fill": 4, "gather": 5, "scatter": 6}
+KERNELS = {"forward": 0, "delta": 1, "dkdv": 2, "dq": 3, "fill": 4, "gather": 5, "scatter": 6,
+           "causal_forward": 7, "causal_delta": 8, "causal_grad": 9, "tree": 10, "append": 11}
 
 
 def kernel_timing_enable(on: bool = True) -> None:
