@@ -318,6 +318,68 @@ sra_status sra_causal_backward(const sra_causal_plan* plan, const void* tables, 
                                const void* o, const float* lse, const void* dout, void* dq, void* dk, void* dv,
                                float softmax_scale, void* workspace, size_t workspace_bytes, void* stream);
 
+/* A paged K/V cache and the sequences of one serving step (§2.3: the audio engine's language model answers token by
+ * token). Pages hold page_size positions of all K/V heads: k and v are bf16 [num_pages, page_size, num_kv_heads,
+ * head_dim] with heads contiguous and a page and a token stride each (0 selects the dense ones). Position p of
+ * sequence b is slot p % page_size of page page_table[b * table_stride + p / page_size].
+ * page_table, context_lens and cu_tokens are DEVICE arrays, read when the call runs: a captured call serves any
+ * values. Sequence b holds context_lens[b] cached positions (taken as 0 below 0, and as max_pages * page_size
+ * above that) and the new tokens cu_tokens[b] .. cu_tokens[b + 1] - 1 of the packed ones (clamped to [0, tokens];
+ * sra_tree_attention also takes a falling entry as equal to the one before). Tokens behind the last sequence's
+ * are padding: their outputs are left as they were. */
+typedef struct sra_paged_cache {
+  int32_t batch;              /* sequences, 1 .. 2048                                       */
+  int32_t tokens;             /* rows of the packed new tokens, >= 0                        */
+  int32_t num_kv_heads;
+  int32_t head_dim;           /* 64 or 128                                                  */
+  int32_t num_pages;          /* >= 1                                                       */
+  int32_t page_size;          /* a power of two, >= 8                                       */
+  int32_t max_pages;          /* entries of a page_table row, >= 1; max_pages * page_size <= 2^30 */
+  void* k;
+  void* v;
+  int64_t k_page_stride, v_page_stride;    /* elements; 0 selects page_size * token stride  */
+  int64_t k_token_stride, v_token_stride;  /* elements; 0 selects num_kv_heads * head_dim   */
+  const int32_t* page_table;
+  int64_t table_stride;       /* entries between rows, >= max_pages; 0 selects max_pages    */
+  const int32_t* context_lens;  /* [batch]     */
+  const int32_t* cu_tokens;     /* [batch + 1] */
+} sra_paged_cache;
+
+/* Bytes of device workspace of sra_tree_attention (library infrastructure). Host only; the pointers of `c` are not
+ * looked at. */
+sra_status sra_tree_workspace_size(const sra_paged_cache* c, int32_t num_heads, size_t* bytes);
+
+/* Attention of each sequence's new tokens (§2.3; one token, or a tree of drafted ones that are checked in one pass): a
+ * token sees its sequence's whole cached context and, of the sequence's new tokens, those that its mask names, through
+ * one softmax (as §4.3 joins cached K/V with the current tokens'). Nothing is written to the cache.
+ * q, o: bf16 [tokens, num_heads, head_dim], k, v: the new tokens' bf16 [tokens, num_kv_heads, head_dim].
+ * tree: device [tokens], bit j of token i's mask = it sees new token j (< 64) of its sequence; itself only if that bit
+ *   is set, and later tokens of a longer sequence are seen by none. NULL: a chain of any length, each token sees the
+ *   new tokens of its sequence up to itself.
+ * Positions of pages whose id is not in [0, num_pages) are seen by no token.
+ * Deterministic; enqueues kernels only. The order of sums follows all lengths of the call. workspace: 256-byte aligned,
+ * as sra_tree_workspace_size says, no initialisation; calls that may overlap need one each. */
+sra_status sra_tree_attention(const sra_paged_cache* c, int32_t num_heads, const void* q, const void* k,
+                              const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                              const uint64_t* tree, void* o, float* lse, float softmax_scale, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/* Writes K and V of new tokens (§2.3; a prompt's, or the accepted ones of a drafted tree) behind their sequences'
+ * context: token i of sequence b goes to position context_lens[b] + i - cu_tokens[b]. k, v: bf16 [n_rows,
+ * num_kv_heads, head_dim]; rows: device [tokens], the row of k and v that each token is (NULL: token i is row i, and
+ * n_rows = tokens). context_lens is not changed: the caller adds the tokens' number when it wants them seen.
+ * Tokens whose position lies behind the page_table row or in a page whose id is not in [0, num_pages), or whose row
+ * is not in [0, n_rows), are skipped. Two tokens of a call never share a position of a sequence; where page_table
+ * names a page twice, which of its writers' rows a slot ends up with is not defined. */
+sra_status sra_cache_append(const sra_paged_cache* c, const void* k, const void* v, int64_t k_stride,
+                            int64_t v_stride, const int32_t* rows, int32_t n_rows, void* stream);
+
+/* Host-only inspection hook of the two calls above (§2.3), with the arrays of `c` in HOST memory (k and v are not looked
+ * at): append_rows[i] = the cache row (page * page_size + slot) that token i is written to, or -1 (rows are taken as
+ * valid), and context_rows[p] = the cache row of position p of sequence `sequence`, or -1 where no token sees it;
+ * either may be NULL. context_rows holds max_pages * page_size entries. */
+sra_status sra_cache_rows(const sra_paged_cache* c, int64_t* append_rows, int32_t sequence, int64_t* context_rows);
+
 /* ---- per-kernel timing (tracing hook; library infrastructure, no passage of the paper) --- */
 
 /* Kernels of the library, for sra_kernel_timing. */

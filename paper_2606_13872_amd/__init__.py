@@ -19,4 +19,5 @@ from .sra import (  # noqa: F401
     schedule_mask,
     useful_flops,
 )
+from .cache import cache_append, cache_rows, tree_attention  # noqa: F401
 from .causal import CausalPlan, causal_backward, causal_forward  # noqa: F401

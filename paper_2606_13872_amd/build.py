@@ -20,7 +20,7 @@ LIB = os.path.join(PKG, "libsra.so")
 
 SOURCES = ["schedule.cpp", "sra_api.cpp", "sra_fwd.hip", "sra_fwd32.hip", "sra_bwd.hip", "sra_grad.hip",
            "sra_compact.hip", "sra_noalloc.hip", "causal_plan.cpp", "sra_text_api.cpp", "sra_causal_fwd.hip",
-           "sra_causal_bwd.hip"]
+           "sra_causal_bwd.hip", "sra_tree.hip"]
 HIP_HOST = ("sra_api.cpp", "sra_text_api.cpp")  # host code that includes the HIP runtime's headers
 
 COMMON = [
@@ -33,7 +33,8 @@ HIP_FLAGS = ["-x", "hip", "--offload-arch=gfx950", "-Xclang", "-target-feature",
 # The dK/dV and dQ kernels (sra_grad.hip, sra_causal_bwd.hip) select their compiler-visible MFMAs in VGPR form: their AGPRs hold
 # the gradient sums (written by inline-assembly MFMAs), and S/dP must stay in VGPRs next to them.
 _VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
-EXTRA_FLAGS = {"sra_grad.hip": _VGPR_FORM, "sra_causal_bwd.hip": _VGPR_FORM}
+# The tree kernel (sra_tree.hip) rescales its sums between MFMAs, so they stay in VGPRs as well.
+EXTRA_FLAGS = {"sra_grad.hip": _VGPR_FORM, "sra_causal_bwd.hip": _VGPR_FORM, "sra_tree.hip": _VGPR_FORM}
 COMPILE_TIMEOUT_S = 900
 
 

@@ -42,10 +42,12 @@ struct CausalTiles {
 struct CausalTile {
   int32_t hg, tok;  // head of the group, first token
 };
+#ifndef SRA_HD
 #ifdef __HIPCC__
 #define SRA_HD __host__ __device__
 #else
 #define SRA_HD
+#endif
 #endif
 SRA_HD inline CausalTiles causal_tiles(const CausalItem& it) {
   const int32_t off = it.nk - it.nq;

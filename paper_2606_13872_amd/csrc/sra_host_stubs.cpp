@@ -4,6 +4,7 @@
 // hipErrorNotSupported, so a call that gets past validation fails with SRA_ERR_HIP.
 #include "sra_causal_kernels.h"
 #include "sra_kernels.h"
+#include "sra_tree.h"
 
 namespace sra {
 
@@ -28,5 +29,7 @@ hipError_t launch_causal_grad(const CausalArgs&, int, int, hipStream_t) { return
 hipError_t launch_causal_grad_combine(const CausalArgs&, const CausalItem*, int, int, hipStream_t) {
   return hipErrorNotSupported;
 }
+hipError_t launch_tree(const TreeArgs&, int, int, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_append(const AppendArgs&, hipStream_t) { return hipErrorNotSupported; }
 
 }  // namespace sra

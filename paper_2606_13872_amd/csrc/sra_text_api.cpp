@@ -1,4 +1,4 @@
-// C ABI of causal attention over packed prompts (include/sra.h): validation, plans and launches.
+// C ABI of causal attention over packed prompts and of the paged cache (include/sra.h): validation, plans, launches.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -10,6 +10,7 @@
 #include "sra.h"
 #include "sra_causal_kernels.h"
 #include "sra_internal.h"
+#include "sra_tree.h"
 
 struct sra_causal_plan {
   sra::CausalTables t;
@@ -104,6 +105,77 @@ sra_status causal_args(const sra_causal_plan* plan, const void* tables, const vo
 
 const CausalItem* table(const sra_causal_plan* p, const void* tables, int i) {
   return reinterpret_cast<const CausalItem*>(static_cast<const char*>(tables) + p->offset[i]);
+}
+
+// Checks of a paged cache (pointers == false: of its sizes alone) and the kernels' view of it.
+sra_status check_cache(const sra_paged_cache* c, bool pointers, bool tensors, PagedCache* out) {
+  if (!c) return fail(SRA_ERR_INVALID_ARGUMENT, "cache is NULL");
+  sra_status st = check_heads(c->num_kv_heads, c->num_kv_heads, c->head_dim);
+  if (st != SRA_OK) return st;
+  if (c->batch < 1 || c->tokens < 0 || c->num_pages < 1 || c->max_pages < 1)
+    return fail(SRA_ERR_INVALID_ARGUMENT, "batch, num_pages and max_pages must be positive, tokens not negative");
+  if (c->batch > kTreeMaxBatch) return fail(SRA_ERR_UNSUPPORTED, "batch must be at most " + std::to_string(kTreeMaxBatch));
+  if (c->page_size < 8 || (c->page_size & (c->page_size - 1)))
+    return fail(SRA_ERR_INVALID_ARGUMENT, "page_size must be a power of two of at least 8");
+  if (int64_t(c->max_pages) * c->page_size > (int64_t(1) << 30))
+    return fail(SRA_ERR_UNSUPPORTED, "max_pages * page_size must be at most 2^30");
+  if (int64_t(c->tokens) * c->num_kv_heads > kMaxInt) return fail(SRA_ERR_UNSUPPORTED, "heads * tokens must be below 2^31");
+  out->k = static_cast<__bf16*>(c->k);
+  out->v = static_cast<__bf16*>(c->v);
+  out->k_token = c->k_token_stride;
+  out->v_token = c->v_token_stride;
+  if ((st = check_stride(&out->k_token, c->num_kv_heads, c->head_dim, "k token")) != SRA_OK) return st;
+  if ((st = check_stride(&out->v_token, c->num_kv_heads, c->head_dim, "v token")) != SRA_OK) return st;
+  out->k_page = c->k_page_stride ? c->k_page_stride : out->k_token * c->page_size;
+  out->v_page = c->v_page_stride ? c->v_page_stride : out->v_token * c->page_size;
+  const int64_t row = int64_t(c->num_kv_heads) * c->head_dim;
+  if (out->k_page < out->k_token * (c->page_size - 1) + row || out->v_page < out->v_token * (c->page_size - 1) + row ||
+      out->k_page % 8 || out->v_page % 8)
+    return fail(SRA_ERR_INVALID_ARGUMENT, "page strides must be multiples of 8 and hold a page");
+  if (out->k_page > (int64_t(1) << 40) || out->v_page > (int64_t(1) << 40))
+    return fail(SRA_ERR_UNSUPPORTED, "a page stride is too large");
+  out->table_stride = c->table_stride ? c->table_stride : c->max_pages;
+  if (out->table_stride < c->max_pages) return fail(SRA_ERR_INVALID_ARGUMENT, "table_stride must be at least max_pages");
+  out->table = c->page_table;
+  out->context_lens = c->context_lens;
+  out->cu_tokens = c->cu_tokens;
+  if (pointers && (!c->page_table || !c->context_lens || !c->cu_tokens || misaligned(c->page_table, 4) ||
+                   misaligned(c->context_lens, 4) || misaligned(c->cu_tokens, 4)))
+    return fail(SRA_ERR_INVALID_ARGUMENT, "page_table, context_lens and cu_tokens must be given, 4-byte aligned");
+  if (tensors && (st = check_pointers({c->k, c->v})) != SRA_OK) return st;
+  out->batch = c->batch;
+  out->tokens = c->tokens;
+  out->pages = c->num_pages;
+  out->page_shift = __builtin_ctz(uint32_t(c->page_size));
+  out->max_pages = c->max_pages;
+  out->kv_heads = c->num_kv_heads;
+  return SRA_OK;
+}
+
+// 16-row blocks per group of rows: as many as a sequence's (token, head of the group) rows fill on average. More would
+// leave the matrix instructions' columns empty, fewer read K and V once for each of several groups.
+int tree_blocks(const sra_paged_cache& c, int32_t heads) {
+  const int64_t rows = (int64_t(c.tokens) + c.batch - 1) / c.batch * (heads / c.num_kv_heads);
+  return rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+}
+
+size_t tree_slots_bytes(int nq, int32_t head_dim) {
+  return align_up(size_t(2) * kTreeGroups * 16 * nq * (head_dim + 2) * 4);
+}
+
+sra_status check_tree(const sra_paged_cache* c, int32_t num_heads, bool pointers, PagedCache* out, size_t* bytes) {
+  sra_status st = check_cache(c, pointers, pointers, out);
+  if (st != SRA_OK) return st;
+  if ((st = check_heads(num_heads, c->num_kv_heads, c->head_dim)) != SRA_OK) return st;
+  if (int64_t(c->tokens) * num_heads > kMaxInt) return fail(SRA_ERR_UNSUPPORTED, "heads * tokens must be below 2^31");
+  const int nq = tree_blocks(*c, num_heads);
+  // the launch's chunks are counted in 32 bits
+  const int64_t keys = int64_t(c->max_pages) * c->page_size / kTreeChunk + c->tokens / kTreeChunk + 2;
+  const int64_t groups = c->batch + int64_t(c->tokens) * (num_heads / c->num_kv_heads) / (16 * nq);
+  if (double(keys) * double(groups) * c->num_kv_heads > double(kMaxInt))
+    return fail(SRA_ERR_UNSUPPORTED, "the tokens times the cache's reach are too many for one call");
+  *bytes = tree_slots_bytes(nq, c->head_dim) + align_up(kTreeGroups * sizeof(TreeSplit));
+  return SRA_OK;
 }
 
 }  // namespace
@@ -288,6 +360,97 @@ sra_status sra_causal_backward(const sra_causal_plan* plan, const void* tables, 
     return launch_causal_grad_combine(a, table(plan, tables, 3), int(t.grad_combine.size()), t.head_dim, s);
   });
   return e == hipSuccess ? SRA_OK : hip_fail(e, "causal gradient launch");
+}
+
+sra_status sra_tree_workspace_size(const sra_paged_cache* c, int32_t num_heads, size_t* bytes) {
+  set_error(SRA_OK, "");
+  if (!bytes) return fail(SRA_ERR_INVALID_ARGUMENT, "bytes is NULL");
+  PagedCache view{};
+  return check_tree(c, num_heads, false, &view, bytes);
+}
+
+sra_status sra_tree_attention(const sra_paged_cache* c, int32_t num_heads, const void* q, const void* k,
+                              const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                              const uint64_t* tree, void* o, float* lse, float softmax_scale, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+  set_error(SRA_OK, "");
+  TreeArgs a{};
+  size_t need = 0;
+  sra_status st = check_tree(c, num_heads, true, &a.c, &need);
+  if (st != SRA_OK) return st;
+  if ((st = check_stride(&q_stride, num_heads, c->head_dim, "q")) != SRA_OK) return st;
+  if ((st = check_stride(&k_stride, c->num_kv_heads, c->head_dim, "k")) != SRA_OK) return st;
+  if ((st = check_stride(&v_stride, c->num_kv_heads, c->head_dim, "v")) != SRA_OK) return st;
+  if (!(softmax_scale == softmax_scale) || softmax_scale > 3.0e38f)
+    return fail(SRA_ERR_INVALID_ARGUMENT, "softmax_scale must be finite");
+  if (c->tokens == 0) return SRA_OK;
+  if ((st = check_pointers({q, k, v, o, lse})) != SRA_OK) return st;
+  if (misaligned(tree, 8)) return fail(SRA_ERR_INVALID_ARGUMENT, "tree must be 8-byte aligned");
+  if ((st = check_workspace(workspace, workspace_bytes, need)) != SRA_OK) return st;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  const int nq = tree_blocks(*c, num_heads);
+  a.q = static_cast<const __bf16*>(q);
+  a.k = static_cast<const __bf16*>(k);
+  a.v = static_cast<const __bf16*>(v);
+  a.qs = q_stride;
+  a.ks = k_stride;
+  a.vs = v_stride;
+  a.tree = tree;
+  a.o = static_cast<__bf16*>(o);
+  a.lse = lse;
+  a.heads = num_heads;
+  a.scale_log2 = float(double(scale_of(softmax_scale, c->head_dim)) * 1.4426950408889634);
+  a.part = static_cast<float*>(workspace);
+  a.split = reinterpret_cast<TreeSplit*>(static_cast<char*>(workspace) + tree_slots_bytes(nq, c->head_dim));
+  const hipError_t e = timed_launch(SRA_KERNEL_TREE, s, [&] { return launch_tree(a, nq, c->head_dim, s); });
+  return e == hipSuccess ? SRA_OK : hip_fail(e, "tree attention launch");
+}
+
+sra_status sra_cache_append(const sra_paged_cache* c, const void* k, const void* v, int64_t k_stride,
+                            int64_t v_stride, const int32_t* rows, int32_t n_rows, void* stream) {
+  set_error(SRA_OK, "");
+  AppendArgs a{};
+  sra_status st = check_cache(c, true, true, &a.c);
+  if (st != SRA_OK) return st;
+  if ((st = check_stride(&k_stride, c->num_kv_heads, c->head_dim, "k")) != SRA_OK) return st;
+  if ((st = check_stride(&v_stride, c->num_kv_heads, c->head_dim, "v")) != SRA_OK) return st;
+  if (n_rows < 0 || (!rows && n_rows != c->tokens))
+    return fail(SRA_ERR_INVALID_ARGUMENT, "without rows, k and v must have one row per token");
+  if (misaligned(rows, 4)) return fail(SRA_ERR_INVALID_ARGUMENT, "rows must be 4-byte aligned");
+  if (c->tokens == 0 || n_rows == 0) return SRA_OK;
+  if ((st = check_pointers({k, v})) != SRA_OK) return st;
+  hipStream_t s = static_cast<hipStream_t>(stream);
+  a.k = static_cast<const __bf16*>(k);
+  a.v = static_cast<const __bf16*>(v);
+  a.ks = k_stride;
+  a.vs = v_stride;
+  a.rows = rows;
+  a.n_rows = n_rows;
+  a.row_elems = c->num_kv_heads * c->head_dim;
+  const hipError_t e = timed_launch(SRA_KERNEL_APPEND, s, [&] { return launch_append(a, s); });
+  return e == hipSuccess ? SRA_OK : hip_fail(e, "cache append launch");
+}
+
+sra_status sra_cache_rows(const sra_paged_cache* c, int64_t* append_rows, int32_t sequence, int64_t* context_rows) {
+  set_error(SRA_OK, "");
+  PagedCache p{};
+  sra_status st = check_cache(c, true, false, &p);
+  if (st != SRA_OK) return st;
+  if (context_rows && (sequence < 0 || sequence >= p.batch)) return fail(SRA_ERR_INVALID_ARGUMENT, "sequence out of range");
+  auto cache_row = [&](int32_t b, int64_t pos) -> int64_t {
+    const int64_t id = pos < 0 ? -1 : cache_page(p, b, pos);
+    return id < 0 ? -1 : (id << p.page_shift) + (pos & (c->page_size - 1));
+  };
+  if (append_rows)
+    for (int32_t i = 0; i < p.tokens; ++i) {
+      int32_t b = 0;
+      while (b < p.batch && p.cu_tokens[b + 1] <= i) ++b;
+      append_rows[i] = b < p.batch ? cache_row(b, append_position(p, b, i)) : -1;
+    }
+  if (context_rows)
+    for (int64_t pos = 0; pos < int64_t(p.max_pages) << p.page_shift; ++pos)
+      context_rows[pos] = pos < cache_context(p, sequence) ? cache_row(sequence, pos) : -1;
+  return SRA_OK;
 }
 
 }  // extern "C"

@@ -1,0 +1,86 @@
+// Argument blocks and launchers of the attention of drafted tokens over a paged cache, and of appending to it.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace sra {
+
+constexpr int kTreeMaxBatch = 2048;  // sequences: their bounds sit in LDS
+constexpr int kTreeChunk = 32;       // keys a wave takes at a time
+constexpr int kTreeGroups = 256;     // workgroups of a launch: one per compute unit, whose LDS it takes
+constexpr int kTreeMinChunks = 8;    // a workgroup takes at least so many chunks: two per wave
+
+#ifndef SRA_HD
+#ifdef __HIPCC__
+#define SRA_HD __host__ __device__
+#else
+#define SRA_HD
+#endif
+#endif
+
+// A group of rows whose keys were split over workgroups, written by the one that has its first keys.
+struct TreeSplit {
+  int32_t pieces;  // 0: none
+  int32_t slot0;   // of the first piece; piece i > 0 is in slot 2 (workgroup + i)
+  int32_t tok0;    // packed token of the sequence's first
+  int32_t row0;    // first (token, head of the group) row of the sequence
+  int32_t rows;
+  int32_t kvh;
+};
+
+struct PagedCache {
+  __bf16 *k, *v;
+  int64_t k_page, v_page, k_token, v_token;  // strides in elements
+  const int32_t* table;                      // [batch] rows of table_stride page ids
+  int64_t table_stride;
+  const int32_t* context_lens;               // [batch]
+  const int32_t* cu_tokens;                  // [batch + 1]
+  int32_t batch, tokens, pages, page_shift, max_pages, kv_heads;
+};
+
+// Cached positions of sequence b.
+SRA_HD inline int32_t cache_context(const PagedCache& c, int32_t b) {
+  const int64_t room = int64_t(c.max_pages) << c.page_shift, n = c.context_lens[b];
+  return int32_t(n < 0 ? 0 : n < room ? n : room);
+}
+// Page of position pos of sequence b, or -1. pos >= 0.
+SRA_HD inline int32_t cache_page(const PagedCache& c, int32_t b, int64_t pos) {
+  const int64_t i = pos >> c.page_shift;
+  if (i >= c.max_pages) return -1;
+  const int32_t id = c.table[int64_t(b) * c.table_stride + i];
+  return id >= 0 && id < c.pages ? id : -1;
+}
+// Position that token i of sequence b is appended at, or -1 where it is not b's.
+SRA_HD inline int64_t append_position(const PagedCache& c, int32_t b, int32_t i) {
+  const int64_t pos = int64_t(c.context_lens[b] > 0 ? c.context_lens[b] : 0) + i;
+  const int32_t first = c.cu_tokens[b] > 0 ? c.cu_tokens[b] : 0;
+  return i < first ? -1 : pos - first;
+}
+
+struct TreeArgs {
+  PagedCache c;
+  const __bf16 *q, *k, *v;  // [tokens, heads, D], [tokens, kv_heads, D]
+  int64_t qs, ks, vs;
+  const uint64_t* tree;     // [tokens] or null: a chain
+  __bf16* o;                // dense
+  float* lse;               // [heads, tokens]
+  int32_t heads;
+  float scale_log2;
+  float* part;              // [2 kTreeGroups] slots: O [16 NQ, D], then (m, l) per row
+  TreeSplit* split;         // [kTreeGroups]
+};
+
+struct AppendArgs {
+  PagedCache c;
+  const __bf16 *k, *v;      // [rows, kv_heads, D]
+  int64_t ks, vs;
+  const int32_t* rows;      // [tokens] or null: row of each token
+  int32_t n_rows;
+  int32_t row_elems;        // kv_heads * D
+};
+
+// nq: 16-row blocks per group of rows (1, 2 or 4)
+hipError_t launch_tree(const TreeArgs& a, int nq, int head_dim, hipStream_t stream);
+hipError_t launch_append(const AppendArgs& a, hipStream_t stream);
+
+}  // namespace sra

@@ -1,0 +1,345 @@
+"""Attention of drafted tokens over a paged cache, and appending to it, on the GPU against their float64 definitions,
+within the bounds of their roundings (oracle/text_oracle.py)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2606_13872_amd as sra
+from oracle import text_oracle as T
+
+pytestmark = pytest.mark.gpu
+INF = float("inf")
+
+
+def make(ctx, new, heads, kv, d, page, seed=0, size=2.0, spare=2, pad=0, strided=False, width=None):
+    """A step's tensors. Pages that no sequence names, and the slots behind a context, hold NaN."""
+    rng = np.random.default_rng(seed)
+    g = torch.Generator(device="cuda").manual_seed(seed)
+
+    def normal(*shape):
+        return torch.randn(shape, generator=g, device="cuda").to(torch.bfloat16)
+
+    need = [min((c + t + page - 1) // page, width or 2**31) for c, t in zip(ctx, new)]
+    pages = sum(need) + spare
+    order = rng.permutation(pages)
+    table = np.full((len(ctx), width or max(1, max(need))), -7, dtype=np.int32)  # entries behind a sequence: no page
+    at = 0
+    if strided:  # K and V of a page side by side, tokens with room between them
+        buf = torch.full((pages, 2, page, kv + 1, d), math.nan, dtype=torch.bfloat16, device="cuda")
+        kc, vc = buf[:, 0, :, :kv], buf[:, 1, :, :kv]
+    else:
+        kc = torch.full((pages, page, kv, d), math.nan, dtype=torch.bfloat16, device="cuda")
+        vc = torch.full_like(kc, math.nan)
+    for b, n in enumerate(need):
+        table[b, :n] = order[at:at + n]
+        at += n
+        if ctx[b]:
+            pos = np.arange(ctx[b])
+            ids = torch.from_numpy(table[b][pos // page].astype(np.int64)).cuda()
+            slot = torch.from_numpy(pos % page).cuda()
+            kc[ids, slot], vc[ids, slot] = normal(ctx[b], kv, d), normal(ctx[b], kv, d)
+    cu = np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+    total = int(cu[-1]) + pad
+    masks = np.zeros(total, dtype=np.uint64)
+    for b, t in enumerate(new):
+        for i in range(t):
+            parent = int(rng.integers(-1, i)) if i else -1
+            above = masks[cu[b] + parent] if parent >= 0 else np.uint64(0)
+            masks[cu[b] + i] = above | (np.uint64(1) << np.uint64(i % 64))
+    dev = {n: torch.from_numpy(a).cuda() for n, a in (("page_table", table), ("cu_tokens", cu),
+                                                      ("context_lens", np.array(ctx, dtype=np.int32)))}
+    x = dict(q=normal(total, heads, d) * size, k=normal(total, kv, d), v=normal(total, kv, d), k_cache=kc, v_cache=vc, **dev)
+    return x, torch.from_numpy(masks.view(np.int64)).cuda(), cu.tolist()
+
+
+def check(x, tree, ctx, cu, scale=None):
+    o, lse = sra.tree_attention(**x, tree=tree, scale=scale)
+    masks = None if tree is None else tree.cpu().numpy().view(np.uint64).tolist()
+    val, bound = T.tree(x["q"], x["k"], x["v"], x["k_cache"], x["v_cache"], x["page_table"], ctx, cu, masks, scale)
+    n = cu[-1]
+    for name, got, cut in (("o", o, lambda t: t[:n]), ("lse", lse, lambda t: t[:, :n])):
+        ok, worst = T.within(cut(got), cut(val[name]), cut(bound[name]))
+        assert ok, f"{name}: {worst:.2f} bounds off"
+    return o, lse
+
+
+STEPS = [
+    ([0], [1]),                                     # nothing cached: the token itself
+    ([1, 31, 32, 33], [1, 1, 1, 1]),
+    ([700, 64, 1500, 31], [1, 1, 1, 1]),
+    ([100, 0, 517, 255], [5, 3, 16, 1]),
+    ([40, 999, 7], [64, 33, 50]),                   # trees of up to 64
+    ([300, 20, 0, 90], [2, 0, 0, 4]),               # sequences without new tokens
+    ([5000], [3]),                                  # one sequence over every workgroup
+]
+
+
+@pytest.mark.parametrize("ctx,new", STEPS)
+@pytest.mark.parametrize("heads,kv,d,page", [(8, 2, 128, 16), (4, 4, 64, 8), (5, 1, 128, 64), (6, 2, 64, 32), (16, 1, 128, 128)])
+def test_trees(ctx, new, heads, kv, d, page):
+    print("tree", ctx, new, heads, kv, d, page, flush=True)
+    x, tree, cu = make(ctx, new, heads, kv, d, page, seed=sum(ctx) + heads)
+    check(x, tree, ctx, cu)
+
+
+@pytest.mark.parametrize("new", [[1, 1, 1], [40, 64, 65], [130, 7, 200]])
+@pytest.mark.parametrize("d", [64, 128])
+def test_chains_of_any_length(new, d):
+    print("chain", new, d, flush=True)
+    ctx = [77, 300, 0]
+    x, _, cu = make(ctx, new, 8, 2, d, 16, seed=3)
+    check(x, None, ctx, cu)
+
+
+def test_many_uneven_sequences():
+    """More sequences than a workgroup has threads, contexts from none to thousands."""
+    print("tree many", flush=True)
+    rng = np.random.default_rng(0)
+    ctx = [int(v) for v in np.exp(rng.uniform(0, 7.5, 300))]
+    new = [int(v) for v in rng.integers(0, 4, 300)]
+    x, tree, cu = make(ctx, new, 4, 2, 64, 16, seed=4)
+    check(x, tree, ctx, cu)
+
+
+@pytest.mark.parametrize("scale", [0.5, 0.01])
+def test_scales_and_strided_caches(scale):
+    print("tree strided", scale, flush=True)
+    ctx, new = [200, 63, 5], [4, 1, 9]
+    x, tree, cu = make(ctx, new, 6, 2, 128, 32, seed=5, strided=True, width=11)
+    wide = torch.zeros(14, 9, 128, dtype=torch.bfloat16, device="cuda")
+    wide[:, 1:7] = x["q"]
+    x["q"] = wide[:, 1:7]
+    x["page_table"] = torch.nn.functional.pad(x["page_table"], (0, 5), value=10**9)[:, :11]
+    check(x, tree, ctx, cu, scale)
+
+
+def test_rows_that_see_nothing_and_masks_without_the_token_itself():
+    print("tree masks", flush=True)
+    ctx, new = [0, 50], [3, 3]
+    x, tree, cu = make(ctx, new, 4, 2, 64, 16, seed=6)
+    tree[:] = torch.tensor([0, 1, 0b110, 0, 0b100, -1])
+    o, lse = check(x, tree, ctx, cu)
+    assert bool((o[0] == 0).all()) and bool((lse[:, 0] == -INF).all())
+
+
+def test_pages_outside_the_cache_are_not_seen():
+    """The same result as with those positions masked away; a whole context of them leaves the drafts."""
+    print("tree bad pages", flush=True)
+    ctx, new = [160, 40], [2, 1]
+    x, tree, cu = make(ctx, new, 4, 2, 128, 16, seed=7)
+    good = x["page_table"].clone()
+    x["page_table"][0, 3], x["page_table"][0, 9], x["page_table"][1, :] = -1, 2**31 - 1, x["k_cache"].shape[0]
+    o, lse = sra.tree_attention(**x, tree=tree)
+    keep = [p for p in range(160) if p // 16 not in (3, 9)]
+    kc, vc = (T.gather_cache(x[n], good[0], 160)[keep] for n in ("k_cache", "v_cache"))
+    for b, (ck, cv) in enumerate(((kc, vc), (kc[:0], vc[:0]))):
+        t0, t1 = cu[b], cu[b + 1]
+        see = torch.ones(t1 - t0, ck.shape[0] + t1 - t0, dtype=torch.bool, device="cuda")
+        for i in range(t1 - t0):
+            for j in range(t1 - t0):
+                see[i, ck.shape[0] + j] = bool((int(tree[t0 + i]) >> j) & 1)
+        for h in range(4):
+            k = torch.cat([ck[:, h // 2], x["k"][t0:t1, h // 2]]).double()
+            v = torch.cat([cv[:, h // 2], x["v"][t0:t1, h // 2]]).double()
+            want, want_lse, _, eo, el = T.rows(x["q"][t0:t1, h].double(), k, v, see, 1 / math.sqrt(128))
+            assert T.within(o[t0:t1, h], want, eo)[0] and T.within(lse[h, t0:t1], want_lse, el)[0]
+
+
+def test_lengths_outside_their_range_stay_inside_the_tensors():
+    """Contexts longer than their table row and below 0, offsets outside the packed tokens and falling ones."""
+    print("tree bad lengths", flush=True)
+    x, tree, _ = make([64, 64, 64], [2, 2, 2], 4, 2, 64, 16, seed=8, width=4)
+    full = sra.tree_attention(**x, tree=tree)
+    x["context_lens"][:] = torch.tensor([10**9, 64, 2**31 - 1])  # the row's reach: 64 positions
+    got = sra.tree_attention(**x, tree=tree)
+    assert torch.equal(full[0], got[0]) and torch.equal(full[1], got[1])
+    x["context_lens"][:] = torch.tensor([64, -5, 64])
+    got = sra.tree_attention(**x, tree=tree)
+    assert torch.equal(got[0][:2], full[0][:2]) and bool(torch.isfinite(got[0][2:4].float()).all())
+    x["context_lens"][:] = 64
+    out = {"o": torch.full_like(full[0], 5.0), "lse": torch.full_like(full[1], 5.0)}
+    x["cu_tokens"][:] = torch.tensor([-3, 2, 1, 100])  # sequence 1 has nothing, sequence 2 the rest
+    sra.tree_attention(**x, tree=tree, out=out)
+    assert torch.equal(out["o"][:2], full[0][:2]) and bool((out["o"][2:] != 5).any(-1).all())
+
+
+def test_padding_rows_keep_what_the_buffers_held():
+    print("tree padding", flush=True)
+    ctx, new = [30, 100], [1, 4]
+    x, tree, cu = make(ctx, new, 4, 2, 128, 16, seed=9, pad=11)
+    out = {"o": torch.full((16, 4, 128), 3.0, dtype=torch.bfloat16, device="cuda"), "lse": torch.full((4, 16), 3.0, device="cuda")}
+    sra.tree_attention(**x, tree=tree, out=out)
+    plain = sra.tree_attention(**{**x, "q": x["q"][:5], "k": x["k"][:5], "v": x["v"][:5]}, tree=tree[:5])
+    assert torch.equal(out["o"][:5], plain[0]) and torch.equal(out["lse"][:, :5], plain[1])
+    assert bool((out["o"][5:] == 3).all()) and bool((out["lse"][:, 5:] == 3).all())
+
+
+def test_long_cache_beyond_32_bit_offsets():
+    """Pages at the end of a cache of more than 2^31 elements."""
+    print("tree far pages", flush=True)
+    page, kv, d = 256, 8, 128
+    pages = 2**31 // (page * kv * d) + 9
+    kc = torch.zeros(pages, page, kv, d, dtype=torch.bfloat16, device="cuda")
+    vc = torch.zeros_like(kc)
+    x, tree, cu = make([600, 512], [1, 2], 16, kv, d, page, seed=10)
+    n = x["k_cache"].shape[0]
+    kc[-n:], vc[-n:] = x["k_cache"], x["v_cache"]
+    want = sra.tree_attention(**x, tree=tree)
+    y = {**x, "k_cache": kc, "v_cache": vc, "page_table": torch.where(x["page_table"] >= 0, x["page_table"] + (pages - n), -1)}
+    got = sra.tree_attention(**y, tree=tree)
+    assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+    sra.cache_append(y["k"], y["v"], kc, vc, y["page_table"], y["context_lens"], y["cu_tokens"])
+    sra.cache_append(x["k"], x["v"], x["k_cache"], x["v_cache"], x["page_table"], x["context_lens"], x["cu_tokens"])
+    for far, near in ((kc, x["k_cache"]), (vc, x["v_cache"])):
+        assert torch.equal(far[-n:].view(torch.int16), near.view(torch.int16))
+        assert not bool(far[:-n].any())
+
+
+@pytest.mark.parametrize("picked", [False, True])
+@pytest.mark.parametrize("kv,d,page,strided", [(2, 64, 8, False), (8, 128, 16, True), (1, 128, 64, False), (3, 64, 32, True)])
+def test_append(picked, kv, d, page, strided):
+    print("append", picked, kv, d, page, strided, flush=True)
+    ctx, new = [0, 31, 100, 7, 16], [3, 40, 0, 1, 90]
+    x, _, cu = make(ctx, new, kv, kv, d, page, seed=11, strided=strided)
+    k, v, rows = x["k"], x["v"], None
+    if picked:
+        k, v = (torch.randn(500, kv, d, device="cuda").to(torch.bfloat16) for _ in range(2))
+        rows = torch.randperm(500, device="cuda")[:cu[-1]].int()
+        rows[5], rows[7] = -1, 500  # no such rows: skipped
+    before = [x["k_cache"].clone(), x["v_cache"].clone()]
+    sra.cache_append(k, v, x["k_cache"], x["v_cache"], x["page_table"], x["context_lens"], x["cu_tokens"], rows=rows)
+    table = x["page_table"].cpu().numpy()
+    for b in range(len(ctx)):
+        for i in range(new[b]):
+            tok, pos = cu[b] + i, ctx[b] + i
+            r = tok if rows is None else int(rows[tok])
+            if 0 <= r < k.shape[0]:
+                for want, src in zip(before, (k, v)):
+                    want[int(table[b, pos // page]), pos % page] = src[r]
+    for got, want in zip((x["k_cache"], x["v_cache"]), before):
+        assert torch.equal(got.contiguous().view(torch.int16), want.contiguous().view(torch.int16))
+
+
+def test_append_skips_what_has_no_place():
+    print("append places", flush=True)
+    x, _, cu = make([10, 20], [4, 4], 2, 2, 64, 16, seed=12, width=2, pad=3)
+    x["page_table"][0, 0], x["page_table"][1, 1] = 10**6, -1
+    x["context_lens"][0] = 30  # positions 30, 31 exist, 32 and 33 do not
+    before = [x["k_cache"].clone(), x["v_cache"].clone()]
+    first = int(x["page_table"][0, 1]) if int(x["page_table"][0, 1]) >= 0 else 0
+    x["page_table"][0, 1] = first
+    sra.cache_append(x["k"], x["v"], x["k_cache"], x["v_cache"], x["page_table"], x["context_lens"], x["cu_tokens"])
+    dst, _ = sra.cache_rows(x["k_cache"].cpu(), x["v_cache"].cpu(), *(x[n].cpu() for n in ("page_table", "context_lens", "cu_tokens")),
+                            tokens=11)
+    assert dst[:4].tolist() == [first * 16 + 14, first * 16 + 15, -1, -1] and (dst[8:] == -1).all()
+    for want, src in zip(before, (x["k"], x["v"])):
+        for i, r in enumerate(dst.tolist()):
+            if r >= 0:
+                want[r // 16, r % 16] = src[i]
+    for got, want in zip((x["k_cache"], x["v_cache"]), before):
+        assert torch.equal(got.view(torch.int16), want.view(torch.int16))
+
+
+def test_repeats_streams_and_guards():
+    """Bitwise equal on every call and stream, and nothing written outside the outputs."""
+    print("tree repeats", flush=True)
+    ctx, new = [1000, 3, 400], [7, 1, 20]
+    x, tree, cu = make(ctx, new, 8, 2, 128, 16, seed=13)
+    o, lse = sra.tree_attention(**x, tree=tree)
+    buf, lbuf = torch.full((o.numel() + 2048,), 9.0, dtype=o.dtype, device="cuda"), torch.full((lse.numel() + 2048,), 9.0, device="cuda")
+    out = {"o": buf[1024:-1024].view(o.shape), "lse": lbuf[1024:-1024].view(lse.shape)}
+    torch.cuda.synchronize()
+    res = []
+    for _ in range(3):
+        for s in (torch.cuda.Stream(), torch.cuda.Stream()):
+            with torch.cuda.stream(s):
+                res.append(sra.tree_attention(**x, tree=tree))
+    torch.cuda.synchronize()
+    sra.tree_attention(**x, tree=tree, out=out)
+    for a, b in res + [(out["o"], out["lse"])]:
+        assert torch.equal(a, o) and torch.equal(b, lse)
+    for t in (buf, lbuf):
+        assert bool((t[:1024] == 9).all()) and bool((t[-1024:] == 9).all())
+
+
+def test_serving_loop_captured_and_eager():
+    """Prompt -> cache -> drafted trees -> accepted tokens, as a server runs them: the step's attention and append are
+    captured once (with padding rows) and replayed with other lengths, and each result is checked against causal
+    attention's float64 definition of the tokens accepted so far."""
+    print("serving loop", flush=True)
+    heads, kv, d, page = 8, 2, 64, 16
+    prompts = [33, 5, 90]
+    g = torch.Generator(device="cuda").manual_seed(14)
+
+    def normal(*shape):
+        return torch.randn(shape, generator=g, device="cuda").to(torch.bfloat16)
+
+    kc, vc = (torch.zeros(60, page, kv, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    table = torch.randperm(60, generator=g, device="cuda")[:36].int().view(3, 12)
+    ctx = torch.zeros(3, dtype=torch.int32, device="cuda")
+    # the prompts
+    q, k, v = normal(sum(prompts), heads, d), normal(sum(prompts), kv, d), normal(sum(prompts), kv, d)
+    plan = sra.CausalPlan(prompts, heads, kv, d, backward=False)
+    o, _ = sra.causal_forward(q, k, v, plan)
+    cu = torch.tensor(np.concatenate([[0], np.cumsum(prompts)]), dtype=torch.int32, device="cuda")
+    sra.cache_append(k, v, kc, vc, table, ctx, cu)
+    chain, _ = sra.tree_attention(q, k, v, kc, vc, table, ctx, cu)  # a prompt is also a chain over an empty context
+    val, bound = T.causal(q, k, v, prompts, prompts)
+    for got in (o, chain):
+        assert T.within(got, val["o"], bound["o"])[0]
+    ctx += torch.tensor(prompts, dtype=torch.int32, device="cuda")
+    hist = [(k[a:b], v[a:b]) for a, b in zip(cu.tolist()[:-1], cu.tolist()[1:])]
+
+    room = 24  # packed rows of a step, padding among them
+    sq, sk, sv = normal(room, heads, d), normal(room, kv, d), normal(room, kv, d)
+    stree = torch.zeros(room, dtype=torch.int64, device="cuda")
+    scu, acu = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    rows = torch.zeros(room, dtype=torch.int32, device="cuda")
+    args = (kc, vc, table, ctx)
+    sra.tree_attention(sq, sk, sv, *args, scu, tree=stree)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        so, slse = sra.tree_attention(sq, sk, sv, *args, scu, tree=stree)
+        sra.cache_append(sk, sv, *args, acu, rows=rows)
+        ctx += acu[1:] - acu[:-1]
+    rng = np.random.default_rng(15)
+    for step in range(6):
+        new = [int(n) for n in rng.integers(1, 8, 3)]
+        cu_h = np.concatenate([[0], np.cumsum(new)])
+        masks, accepted, picked = [0] * room, [], []
+        for b, t in enumerate(new):
+            paths = []
+            for i in range(t):
+                parent = int(rng.integers(-1, i)) if i else -1
+                paths.append((paths[parent] if parent >= 0 else []) + [i])
+                masks[cu_h[b] + i] = sum(1 << j for j in paths[-1])
+            path = paths[int(rng.integers(0, t))]
+            accepted.append(len(path))
+            picked += [int(cu_h[b]) + j for j in path]
+        for dst, src in ((sq, normal(room, heads, d)), (sk, normal(room, kv, d)), (sv, normal(room, kv, d)),
+                         (stree, torch.tensor(masks)), (scu, torch.from_numpy(cu_h.astype(np.int32))),
+                         (acu, torch.from_numpy(np.concatenate([[0], np.cumsum(accepted)]).astype(np.int32))),
+                         (rows, torch.tensor(picked + [0] * (room - len(picked)), dtype=torch.int32))):
+            dst.copy_(src)
+        ctx_h = ctx.tolist()
+        eager = sra.tree_attention(sq, sk, sv, *args, scu, tree=stree)
+        graph.replay()
+        torch.cuda.synchronize()
+        n = int(cu_h[-1])
+        assert torch.equal(eager[0][:n], so[:n]) and torch.equal(eager[1][:, :n], slse[:, :n])
+        assert ctx.tolist() == [c + a for c, a in zip(ctx_h, accepted)]
+        at = 0
+        for b, t in enumerate(new):  # the accepted path of each sequence is the end of a causal sequence
+            path = [p - int(cu_h[b]) for p in picked[at:at + accepted[b]]]
+            at += accepted[b]
+            sel = torch.tensor([int(cu_h[b]) + j for j in path], device="cuda")
+            hk, hv = torch.cat([hist[b][0], sk[sel]]), torch.cat([hist[b][1], sv[sel]])
+            val, bound = T.causal(sq[sel], hk, hv, [len(path)], [hk.shape[0]])
+            ok, worst = T.within(so[sel], val["o"], bound["o"])
+            assert ok, (step, b, worst)
+            hist[b] = (hk, hv)
+            for cache, want in ((kc, hk), (vc, hv)):
+                assert torch.equal(T.gather_cache(cache, table[b], want.shape[0]), want)
