@@ -8,7 +8,10 @@ namespace sra {
 constexpr int kTreeMaxBatch = 2048;  // sequences: their bounds sit in LDS
 constexpr int kTreeChunk = 32;       // keys a wave takes at a time
 constexpr int kTreeGroups = 256;     // workgroups of a launch: one per compute unit, whose LDS it takes
-constexpr int kTreeMinChunks = 8;    // a workgroup takes at least so many chunks: two per wave
+// What beginning a group of rows costs a workgroup, in chunks: its bounds, queries, first loads and the merge of the
+// waves are a chain of latencies (about 5 us, the time of as many chunks of four waves when the cache bounds them).
+constexpr int kTreeStart = 8;
+constexpr int kTreeMinRun = kTreeStart + 8;  // a workgroup takes at least so much: two chunks per wave
 
 #ifndef SRA_HD
 #ifdef __HIPCC__
@@ -18,10 +21,10 @@ constexpr int kTreeMinChunks = 8;    // a workgroup takes at least so many chunk
 #endif
 #endif
 
-// A group of rows whose keys were split over workgroups, written by the one that has its first keys.
+// A group of rows whose keys were split over workgroups, written by the one (w) that has its first keys. That piece is
+// in slot 2 w + 1, the others, with which their workgroups begin, in slots 2 (w + i).
 struct TreeSplit {
   int32_t pieces;  // 0: none
-  int32_t slot0;   // of the first piece; piece i > 0 is in slot 2 (workgroup + i)
   int32_t tok0;    // packed token of the sequence's first
   int32_t row0;    // first (token, head of the group) row of the sequence
   int32_t rows;

@@ -5,9 +5,10 @@
 // (token, head of the group) pairs, 16 NQ of them to a group of rows, so that K and V are read once for all of them.
 //
 // Bound by reading the cache: all of the launch's keys, counted in 32-key chunks (of each sequence, K/V head and
-// group of rows, one after the other), are dealt to the workgroups in equal runs, whatever the lengths; a run may end
-// one group of rows and begin another. Lengths are read on the device, so a captured call serves any lengths. A
-// group that several workgroups share is added up by a second kernel, in the order of its keys.
+// group of rows, one after the other, with kTreeStart more for beginning each group), are dealt to the workgroups in
+// equal runs, whatever the lengths; a run may end one group of rows and begin another. Lengths are read on the
+// device, so a captured call serves any lengths. A group that several workgroups share is added up by a second
+// kernel, in the order of its keys.
 //
 // In a workgroup each of the four waves takes every fourth chunk, alone: it loads the chunk's K and V rows into an
 // LDS ring of its own (global -> LDS, the chunks behind it in flight, no barrier), computes S^T = K Q^T, the running maximum and
@@ -31,7 +32,8 @@ __device__ __forceinline__ void wait_vmem_to() {
 }
 
 // Bounds of the sequences: first[b] .. first[b + 1] are b's tokens (cu_tokens clamped into [0, tokens] and never
-// falling, so no token has two sequences), chunk[b] .. chunk[b + 1] its chunks of all K/V heads and groups of rows.
+// falling, so no token has two sequences), chunk[b] .. chunk[b + 1] the costs, in chunks, of its groups of rows of all
+// K/V heads.
 struct TreeBounds {
   int32_t first[kTreeMaxBatch + 1];
   int32_t chunk[kTreeMaxBatch + 1];
@@ -61,7 +63,7 @@ __device__ __forceinline__ void tree_bounds(const TreeArgs& a, TreeBounds& s) {
     f = max(f, carry_first);
     for (int w = 0; w < wave; ++w) f = max(f, s.wave[0][w]);
     const int end = max(f, end_raw), t = end - f;
-    const int chunks = (ctx + kTreeChunk - 1) / kTreeChunk + (t + kTreeChunk - 1) / kTreeChunk;
+    const int chunks = kTreeStart + (ctx + t + kTreeChunk - 1) / kTreeChunk;
     int x = t > 0 ? chunks * ((t * G + 16 * NQ - 1) / (16 * NQ)) * a.c.kv_heads : 0;
 #pragma unroll
     for (int w = 1; w < 64; w <<= 1) {
@@ -89,10 +91,76 @@ __device__ __forceinline__ void tree_bounds(const TreeArgs& a, TreeBounds& s) {
 // Per-wave state of a run over one group of rows.
 template <int D, int NQ>
 struct TreeState {
+  static constexpr bool kAgpr = NQ == 4;  // O in AGPRs (inline-assembly MFMAs): with it the VGPRs would not do
   bf16x8 qf[NQ][D / 32];  // Q^T B fragments (lane = row)
   floatx4 o[NQ][D / 16];
   float m[NQ], l[NQ];     // running maximum (log2 units), this lane's part of the sum
+  // O may be read and written by vector instructions from here on
+  __device__ __forceinline__ void settle() {
+    if constexpr (kAgpr) {
+      mfma_drain();
+#pragma unroll
+      for (int qb = 0; qb < NQ; ++qb)
+#pragma unroll
+        for (int db = 0; db < D / 16; ++db) asm volatile("" : "+a"(o[qb][db]));
+    }
+  }
 };
+
+// P of a chunk against the running maxima m as they are, and the lane's partial sums; false where one is above
+// kTreeBigSum (or m still -inf), so that m has to move.
+constexpr float kTreeBigSum = 65536.0f;
+template <int D, int NQ>
+__device__ __forceinline__ bool tree_soft(const TreeState<D, NQ>& st, const floatx4 (&s)[2][NQ], bf16x8 (&p)[NQ],
+                                          float (&sum)[NQ], float sl2) {
+  bool ok = true;
+#pragma unroll
+  for (int qb = 0; qb < NQ; ++qb) {
+    const float nm = -st.m[qb];
+    float acc = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = fast_exp2(fmaf(s[kb][qb][i], sl2, nm));
+        acc += x;
+        p[qb][4 * kb + i] = (__bf16)x;  // P in bf16 for the matrix product, its sum in 32 bits
+      }
+    sum[qb] = acc;
+    ok = ok && acc <= kTreeBigSum;
+  }
+  return ok;
+}
+
+// Moves m to the true running maxima (rescaling O and l) and computes P and the partial sums against them.
+template <int D, int NQ>
+__device__ __forceinline__ void tree_rescale(TreeState<D, NQ>& st, const floatx4 (&s)[2][NQ], bf16x8 (&p)[NQ],
+                                             float (&sum)[NQ], float sl2) {
+  st.settle();
+#pragma unroll
+  for (int qb = 0; qb < NQ; ++qb) {
+    const floatx4 x = s[0][qb], y = s[1][qb];
+    const float mx = quad_max(max2f(max3f(x[0], x[1], max2f(x[2], x[3])), max3f(y[0], y[1], max2f(y[2], y[3])))) * sl2;
+    if (mx > st.m[qb]) {
+      const float alpha = fast_exp2(st.m[qb] - mx);  // 0 when m was -inf
+      st.m[qb] = mx;
+      st.l[qb] *= alpha;
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db) st.o[qb][db] *= alpha;
+    }
+    const float nm = st.m[qb] == -INFINITY ? 0.f : -st.m[qb];  // a row that has seen nothing keeps P = 0
+    float acc = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float e = fast_exp2(fmaf(s[kb][qb][i], sl2, nm));
+        acc += e;
+        p[qb][4 * kb + i] = (__bf16)e;
+      }
+    sum[qb] = acc;
+  }
+}
 
 // One chunk: K rows at LDS address kt, V rows at vt (waited for between the two by `land_v`). kMasked: key 16 kb + 4 g +
 // i of the chunk is seen by this lane's row of block qb if bit 16 kb + 4 g + i of vis[qb] is set.
@@ -111,44 +179,34 @@ __device__ __forceinline__ void tree_chunk(TreeState<D, NQ>& st, uint32_t kt, ui
       for (int qb = 0; qb < NQ; ++qb) s[kb][qb] = mfma16(k, st.qf[qb][c], c == 0 ? floatx4{} : s[kb][qb]);
     }
   bf16x8 p[NQ];
+  float sum[NQ];
+  bool ok = false;
+  if constexpr (kMasked) {
 #pragma unroll
-  for (int qb = 0; qb < NQ; ++qb) {
-    floatx4 &x = s[0][qb], &y = s[1][qb];
-    if constexpr (kMasked) {
+    for (int qb = 0; qb < NQ; ++qb) {
       const uint32_t w = vis[qb] >> (4 * g);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        x[i] = (w >> i) & 1 ? x[i] : -INFINITY;
-        y[i] = (w >> (16 + i)) & 1 ? y[i] : -INFINITY;
+        s[0][qb][i] = (w >> i) & 1 ? s[0][qb][i] : -INFINITY;
+        s[1][qb][i] = (w >> (16 + i)) & 1 ? s[1][qb][i] : -INFINITY;
       }
     }
-    const float mx = quad_max(max2f(max3f(x[0], x[1], max2f(x[2], x[3])), max3f(y[0], y[1], max2f(y[2], y[3])))) * sl2;
-    if (mx > st.m[qb]) {
-      const float alpha = fast_exp2(st.m[qb] - mx);  // 0 when m was -inf
-      st.m[qb] = mx;
-      st.l[qb] *= alpha;
-#pragma unroll
-      for (int db = 0; db < ND; ++db) st.o[qb][db] *= alpha;
-    }
-    const float nm = st.m[qb] == -INFINITY ? 0.f : -st.m[qb];  // a row that has seen nothing keeps P = 0
-    float acc = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[i] = fast_exp2(fmaf(x[i], sl2, nm));
-      y[i] = fast_exp2(fmaf(y[i], sl2, nm));
-      acc += x[i] + y[i];
-      p[qb][i] = (__bf16)x[i];  // P in bf16 for the matrix product, its sum in 32 bits
-      p[qb][4 + i] = (__bf16)y[i];
-    }
-    st.l[qb] += acc;
+  } else {
+    ok = tree_soft<D, NQ>(st, s, p, sum, sl2);
   }
+  if (kMasked || __builtin_expect(__builtin_amdgcn_ballot_w64(!ok) != 0, 0)) tree_rescale<D, NQ>(st, s, p, sum, sl2);
+#pragma unroll
+  for (int qb = 0; qb < NQ; ++qb) st.l[qb] += sum[qb];
   land_v();
 #pragma unroll
   for (int db = 0; db < ND; ++db) {
     const uint32_t x = (vt + tr) ^ (32 * db);
     const bf16x8 v = cat8(lds_ld_tr(x), lds_ld_tr(x + 32 * D));
 #pragma unroll
-    for (int qb = 0; qb < NQ; ++qb) st.o[qb][db] = mfma16(v, p[qb], st.o[qb][db]);
+    for (int qb = 0; qb < NQ; ++qb) {
+      if constexpr (TreeState<D, NQ>::kAgpr) mfma16_agpr(st.o[qb][db], v, p[qb]);
+      else st.o[qb][db] = mfma16(v, p[qb], st.o[qb][db]);
+    }
   }
 }
 
@@ -172,9 +230,9 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
 
   tree_bounds<NQ>(a, bounds);
   const int total = __builtin_amdgcn_readfirstlane(bounds.chunk[c.batch]);
-  const int run = max(kTreeMinChunks, (total + kTreeGroups - 1) / kTreeGroups);
+  const int run = max(kTreeMinRun, (total + kTreeGroups - 1) / kTreeGroups);
   const int begin = int(min(int64_t(w) * run, int64_t(total))), end = int(min(int64_t(begin) + run, int64_t(total)));
-  TreeSplit split{0, 0, 0, 0, 0, 0};
+  TreeSplit split{0, 0, 0, 0, 0};
 
   const uint32_t ring = lds_addr(lds) + wave * kRing;
   const uint32_t row = swz_row_addr<D>(), tr = swz_tr_addr<D>();
@@ -196,13 +254,82 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
     const int t0 = __builtin_amdgcn_readfirstlane(bounds.first[b]);
     const int t = __builtin_amdgcn_readfirstlane(bounds.first[b + 1]) - t0;
     const int ctx = __builtin_amdgcn_readfirstlane(cache_context(c, b));
-    const int n_ctx = (ctx + kTreeChunk - 1) / kTreeChunk, n = n_ctx + (t + kTreeChunk - 1) / kTreeChunk;
+    const int n = (ctx + t + kTreeChunk - 1) / kTreeChunk;  // keys: the context's, then the new tokens'
     const int blocks = (t * G + R - 1) / R;
-    const int u = x - __builtin_amdgcn_readfirstlane(bounds.chunk[b]), grp = u / n;
-    const int c0 = u - grp * n, c1 = min(n, c0 + end - x);
+    const int u = x - __builtin_amdgcn_readfirstlane(bounds.chunk[b]), cost = kTreeStart + n, grp = u / cost;
+    // chunk i of the group is at origin + i
+    const int origin = x - (u - grp * cost) + kTreeStart, c0 = max(x - origin, 0), c1 = min(n, end - origin);
+    x = origin + n;
+    if (c0 >= c1) continue;  // the run ends before its first chunk
     const int kvh = grp / blocks, row0 = (grp - kvh * blocks) * R, rows = min(R, t * G - row0);
     const const_ints table = (const_ints)(uintptr_t)(c.table + int64_t(b) * c.table_stride);
 
+    // Page ids of chunk i's four groups of 8 rows (a page holds a multiple of 8), where the chunk is all context.
+    struct Ids {
+      int v[4];
+    };
+    auto page_ids = [&](int i) __attribute__((always_inline)) {
+      Ids ids{};
+      if ((i + 1) * kTreeChunk <= ctx) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ids.v[j] = table[(i * kTreeChunk + 8 * j) >> c.page_shift];
+      }
+      return ids;
+    };
+    // Issues chunk i's 2 kInstr loads into stage s; returns which of its 32 keys exist.
+    auto issue = [&](int i, int s, const Ids& ids) __attribute__((always_inline)) -> uint32_t {
+      const uint32_t la = ring + s * 2 * kTile;
+      const int p0 = i * kTreeChunk;
+      if (p0 + kTreeChunk <= ctx) {
+        bool ok = true;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ok = ok && uint32_t(ids.v[j]) < uint32_t(c.pages);
+        if (ok) {
+          constexpr int kPer = kInstr / 4;  // load instructions of 8 rows
+#pragma unroll
+          for (int kv = 0; kv < 2; ++kv) {
+            const __bf16* base = (kv ? c.v : c.k) + int64_t(kvh) * D;
+            const int64_t ps = kv ? c.v_page : c.k_page, ts = kv ? c.v_token : c.k_token;
+            const uint32_t lane_row = uint32_t(lrow * ts);
+#pragma unroll
+            for (int j = 0; j < kInstr; ++j) {
+              const int slot = (p0 + (j / kPer) * 8) & (page_rows - 1);
+              const __bf16* src = base + ids.v[j / kPer] * ps + slot * ts + (j % kPer) * (RPI * ts);
+              lds_dma_x4_off(uniform_u64(reinterpret_cast<uint64_t>(src)), (lane_row + chunk16[j % kKinds]) * 2,
+                             la + kv * kTile + j * 1024);
+            }
+          }
+          return ~0u;
+        }
+      }
+      // the context's end, new tokens, or a page that is none: row by row. Keys that do not exist read a new token of
+      // the sequence instead, a row that is there
+      const int pos = p0 + (lane & 31);
+      const int page = pos < ctx ? cache_page(c, b, pos) : -1;
+      const uint32_t exist = uint32_t(__builtin_amdgcn_ballot_w64(page >= 0 || (pos >= ctx && pos - ctx < t)));
+#pragma unroll 1
+      for (int e = 0; e < 2 * kInstr; ++e) {  // K, then V: the waits below count on that order
+        const int j = e % kInstr, r = j * RPI + lrow, p = p0 + r;
+        const bool is_v = e >= kInstr;
+        const int64_t id = __shfl(page, r, 64), slot = p & (page_rows - 1);
+        const int64_t fresh = t0 + (p < ctx ? 0 : min(p - ctx, t - 1));
+        const __bf16* src = id >= 0 ? (is_v ? c.v : c.k) + id * (is_v ? c.v_page : c.k_page) + slot * (is_v ? c.v_token : c.k_token)
+                                    : (is_v ? a.v : a.k) + fresh * (is_v ? a.vs : a.ks);
+        lds_dma_x4_at(src + kvh * D + ((lane % CPR) ^ swz<D>(r)) * 8, la + is_v * kTile + j * 1024);
+      }
+      return exist;
+    };
+
+    // chunk i + kTreeWaves k sits in stage k % NS; NS - 1 chunks are in flight behind the one that is worked on
+    constexpr int NS = kStages<D>, kAhead = (NS - 1) * kTreeWaves;
+    uint32_t exist[NS];
+#pragma unroll
+    for (int k = 0; k < NS - 1; ++k) {
+      exist[k] = 0;
+      const int i = c0 + wave + k * kTreeWaves;
+      if (i < c1) exist[k] = issue(i, k, page_ids(i));
+    }
+    Ids ids = page_ids(c0 + wave + kAhead);  // of the chunk that is loaded next
     TreeState<D, NQ> st;
     uint64_t tree[NQ];  // which drafted tokens the lane's row sees (a chain: all up to itself; see below)
     int tok[NQ];
@@ -219,7 +346,7 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
       st.m[qb] = -INFINITY;
       st.l[qb] = 0.f;
     }
-    // land them here: the waits inside the loop count the direct loads alone
+    // land them here, behind the first chunks: the waits inside the loop count the direct loads alone
 #pragma unroll
     for (int qb = 0; qb < NQ; ++qb) {
 #pragma unroll
@@ -227,74 +354,14 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
       asm volatile("" : "+v"(tree[qb]));
     }
 
-    // Issues chunk i's 2 kInstr loads into stage s; returns which of its 32 keys exist.
-    auto issue = [&](int i, int s) __attribute__((always_inline)) -> uint32_t {
-      const uint32_t la = ring + s * 2 * kTile;
-      if (i < n_ctx) {
-        const int p0 = i * kTreeChunk;
-        int ids[kInstr];
-        bool ok = p0 + kTreeChunk <= ctx;
-        if (ok) {
-#pragma unroll
-          for (int j = 0; j < kInstr; ++j) ids[j] = table[(p0 + j * RPI) >> c.page_shift];
-#pragma unroll
-          for (int j = 0; j < kInstr; ++j) ok = ok && uint32_t(ids[j]) < uint32_t(c.pages);
-        }
-        if (ok) {
-#pragma unroll
-          for (int kv = 0; kv < 2; ++kv) {
-            const __bf16* base = (kv ? c.v : c.k) + int64_t(kvh) * D;
-            const int64_t ps = kv ? c.v_page : c.k_page, ts = kv ? c.v_token : c.k_token;
-            const uint32_t lane_row = uint32_t(lrow * ts);
-#pragma unroll
-            for (int j = 0; j < kInstr; ++j) {
-              const int slot = (p0 + j * RPI) & (page_rows - 1);
-              lds_dma_x4_off(uniform_u64(reinterpret_cast<uint64_t>(base + ids[j] * ps + slot * ts)),
-                             (lane_row + chunk16[j % kKinds]) * 2, la + kv * kTile + j * 1024);
-            }
-          }
-          return ~0u;
-        }
-      }
-      // drafted tokens, the context's end, or a page that is none: row by row. Keys that do not exist read a new
-      // token of the sequence instead, a row that is there
-      uint32_t exist = 0;
-      const int p0 = i * kTreeChunk, d0 = (i - n_ctx) * kTreeChunk;
-      if (i < n_ctx) {
-        const int pos = p0 + (lane & 31);
-        const bool mine = pos < ctx && cache_page(c, b, pos) >= 0;
-        exist = uint32_t(__builtin_amdgcn_ballot_w64(mine));
-      }
-#pragma unroll 1
-      for (int e = 0; e < 2 * kInstr; ++e) {  // K, then V: the waits below count on that order
-        const int j = e % kInstr, r = j * RPI + lrow;
-        const bool is_v = e >= kInstr;
-        const int64_t fresh = t0 + (i < n_ctx ? 0 : min(d0 + r, t - 1));
-        const __bf16* src = (is_v ? a.v : a.k) + fresh * (is_v ? a.vs : a.ks);
-        if ((exist >> r) & 1) {
-          const int64_t id = table[(p0 + r) >> c.page_shift], slot = (p0 + r) & (page_rows - 1);
-          src = (is_v ? c.v : c.k) + id * (is_v ? c.v_page : c.k_page) + slot * (is_v ? c.v_token : c.k_token);
-        }
-        lds_dma_x4_at(src + kvh * D + ((lane % CPR) ^ swz<D>(r)) * 8, la + is_v * kTile + j * 1024);
-      }
-      return exist;
-    };
-
-    // chunk i + kTreeWaves k sits in stage k % NS; NS - 1 chunks are in flight behind the one that is worked on
-    constexpr int NS = kStages<D>, kAhead = (NS - 1) * kTreeWaves;
-    uint32_t exist[NS];
-#pragma unroll
-    for (int k = 0; k < NS - 1; ++k) {
-      exist[k] = 0;
-      if (c0 + wave + k * kTreeWaves < c1) exist[k] = issue(c0 + wave + k * kTreeWaves, k);
-    }
     int s = 0;
     for (int i = c0 + wave; i < c1; i += kTreeWaves) {
       const bool more = i + kAhead < c1;
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the stage that is loaded next has been read
       exist[NS - 1] = 0;
       if (more) {
-        exist[NS - 1] = issue(i + kAhead, (s + NS - 1) % NS);
+        exist[NS - 1] = issue(i + kAhead, (s + NS - 1) % NS, ids);
+        ids = page_ids(i + kAhead + kTreeWaves);
         // the loads of the chunks behind this one, and this one's V, may be in flight
         wait_vmem_to<(2 * (NS - 1) + 1) * kInstr>();
       } else {
@@ -304,24 +371,23 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
         if (more) wait_vmem_to<2 * (NS - 1) * kInstr>();
       };
       const uint32_t kt = ring + s * 2 * kTile, vt = kt + kTile;
-      if (exist[0] == ~0u) {
+      if (exist[0] == ~0u && (i + 1) * kTreeChunk <= ctx) {
         tree_chunk<D, NQ, false>(st, kt, vt, row, tr, nullptr, sl2, land_v);
       } else {
         uint32_t vis[NQ];
 #pragma unroll
         for (int qb = 0; qb < NQ; ++qb) {
-          if (i < n_ctx) {
-            vis[qb] = exist[0];
+          // bit e is position 32 i + e, new token e - to
+          const int to = ctx - i * kTreeChunk;
+          uint32_t draft;
+          if (a.tree) {
+            draft = to >= 32 ? 0 : to >= 0 ? uint32_t(tree[qb] << to) : to > -64 ? uint32_t(tree[qb] >> -to) : 0;
           } else {
-            const int d0 = (i - n_ctx) * kTreeChunk;
-            if (a.tree) {
-              vis[qb] = d0 < 64 ? uint32_t(tree[qb] >> d0) : 0;
-            } else {
-              const int last = tok[qb] - d0;
-              vis[qb] = last >= 31 ? ~0u : last < 0 ? 0 : (2u << last) - 1;
-            }
-            if (t - d0 < 32) vis[qb] &= (1u << (t - d0)) - 1;
+            const int last = tok[qb] + to;
+            draft = last >= 31 ? ~0u : last < 0 ? 0 : (2u << last) - 1;
           }
+          const uint32_t cached = to >= 32 ? ~0u : to > 0 ? (1u << to) - 1 : 0;
+          vis[qb] = exist[0] & (cached | draft);
         }
         tree_chunk<D, NQ, true>(st, kt, vt, row, tr, vis, sl2, land_v);
       }
@@ -339,6 +405,7 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
         ml[wave][16 * qb + l16][1] = l;
       }
     }
+    st.settle();
     float* const mine = reinterpret_cast<float*>(lds + wave * kRing);
 #pragma unroll
     for (int qb = 0; qb < NQ; ++qb)
@@ -347,7 +414,7 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
         *reinterpret_cast<floatx4*>(mine + (16 * qb + l16) * D + ((4 * db + g) ^ l16) * 4) = st.o[qb][db];
     __syncthreads();
     const bool whole = c0 == 0 && c1 == n;
-    const int slot = 2 * w + (x == begin ? 0 : 1);
+    const int slot = 2 * w + (c0 == 0);
     float* const part = a.part + int64_t(slot) * R * (D + 2);
     for (int e = threadIdx.x; e < rows * (D / 4); e += kTreeThreads) {
       const int r = e / (D / 4), q = e % (D / 4);
@@ -377,8 +444,7 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
       }
     }
     if (!whole && c0 == 0)  // the group's first keys
-      split = TreeSplit{(x + n - 1) / run - w + 1, slot, t0, row0, rows, kvh};
-    x += c1 - c0;
+      split = TreeSplit{(origin + n - 1) / run - w + 1, t0, row0, rows, kvh};
     __syncthreads();  // the rings and ml are free again
   }
   if (threadIdx.x == 0) a.split[w] = split;
@@ -394,7 +460,7 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_combine_kernel(TreeArgs
   const TreeSplit sp = a.split[w];
   const int r = blockIdx.y * RPB + threadIdx.x / TPR, sub = threadIdx.x % TPR;
   if (sp.pieces == 0 || r >= sp.rows) return;
-  auto piece = [&](int i) { return a.part + kSlot * (i == 0 ? sp.slot0 : 2 * (w + i)); };
+  auto piece = [&](int i) { return a.part + kSlot * (2 * (w + i) + (i == 0)); };
   float m = -INFINITY;
   for (int i = 0; i < sp.pieces; ++i) m = fmaxf(m, piece(i)[R * D + 2 * r]);
   floatx4 o = floatx4{};
