@@ -41,25 +41,48 @@ struct Ahead {
   bf16x8 k[kLook], v[kLook];
 };
 
-// K row fragment i of the 32 keys at kt (A operand of S^T = K Q^T): keys 16 kb .. + 15 and head
-// dims 32 c .. + 31, i = (D / 32) kb + c.
-template <int D>
+// How a 64-key LDS tile is laid out: padded rows (PaddedTile) or swizzled ones (SwzTile), whose load instructions hold
+// whole rows. Both read their fragments without bank conflicts at compile-time offsets from a few per-lane addresses.
+// k_frag: K row fragment i of the 32 keys at kt (A operand of S^T = K Q^T): keys 16 kb .. + 15 and head dims
+//   32 c .. + 31, i = (D / 32) kb + c.
+// v_frag: V^T fragment db of the 32 keys at vt (A operand of O^T += V^T P^T): head dims 16 db .. + 15. The transpose
+//   read gives lane (head dim) the 8 keys whose P values the B fragment holds.
+struct PaddedRows {
+  template <int D>
+  static __device__ __forceinline__ bf16x8 k_frag(const __bf16* kt, int i) {
+    const int lane = threadIdx.x & 63, kb = i / (D / 32), c = i % (D / 32);
+    return *reinterpret_cast<const bf16x8*>(kt + ((lane & 15) + 16 * kb) * kPadRS<D> + c * 32 + (lane >> 4) * 8);
+  }
+  template <int D>
+  static __device__ __forceinline__ bf16x8 v_frag(const __bf16* vt, int db) {
+    const int lane = threadIdx.x & 63;
+    const int r0 = 4 * (lane >> 4) + ((lane & 15) >> 2), col = db * 16 + 4 * (lane & 3);
+    return cat8(lds_read_tr(vt + r0 * kPadRS<D> + col), lds_read_tr(vt + (r0 + 16) * kPadRS<D> + col));
+  }
+};
+struct SwizzledRows {
+  template <int D>
+  static __device__ __forceinline__ bf16x8 k_frag(const __bf16* kt, int i) {
+    const int kb = i / (D / 32), c = i % (D / 32);
+    return *reinterpret_cast<const bf16x8*>(kt + kb * 16 * D + (swz_row_addr<D>() ^ (64 * c)) / 2);
+  }
+  template <int D>
+  static __device__ __forceinline__ bf16x8 v_frag(const __bf16* vt, int db) {
+    const uint32_t x = (swz_tr_addr<D>() ^ (32 * db)) / 2;
+    return cat8(lds_read_tr(vt + x), lds_read_tr(vt + 16 * D + x));
+  }
+};
+template <int D, class L = PaddedRows>
 __device__ __forceinline__ bf16x8 k_frag(const __bf16* kt, int i) {
-  const int lane = threadIdx.x & 63, kb = i / (D / 32), c = i % (D / 32);
-  return *reinterpret_cast<const bf16x8*>(kt + ((lane & 15) + 16 * kb) * kPadRS<D> + c * 32 + (lane >> 4) * 8);
+  return L::template k_frag<D>(kt, i);
 }
-
-// V^T fragment db of the 32 keys at vt (A operand of O^T += V^T P^T): head dims 16 db .. + 15.
-// The transpose read gives lane (head dim) the 8 keys whose P values the B fragment holds.
-template <int D>
+template <int D, class L = PaddedRows>
 __device__ __forceinline__ bf16x8 v_frag(const __bf16* vt, int db) {
-  const int lane = threadIdx.x & 63;
-  const int r0 = 4 * (lane >> 4) + ((lane & 15) >> 2), col = db * 16 + 4 * (lane & 3);
-  return cat8(lds_read_tr(vt + r0 * kPadRS<D> + col), lds_read_tr(vt + (r0 + 16) * kPadRS<D> + col));
+  return L::template v_frag<D>(vt, db);
 }
 
 // S^T of 32 keys, plain (used outside the pipeline).
-template <int D, int NQ>
+template <int D, int NQ, class L = PaddedRows>
 __device__ __forceinline__ HalfS<NQ> scores32(const FwdState<D, NQ>& st, const __bf16* kt) {
   HalfS<NQ> s;
 #pragma unroll
@@ -67,7 +90,7 @@ __device__ __forceinline__ HalfS<NQ> scores32(const FwdState<D, NQ>& st, const _
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) {
     const int kb = i / (D / 32), c = i % (D / 32);
-    const bf16x8 k = k_frag<D>(kt, i);
+    const bf16x8 k = k_frag<D, L>(kt, i);
 #pragma unroll
     for (int qb = 0; qb < NQ; ++qb) s.b[NQ * kb + qb] = mfma16(k, st.qf[qb][c], s.b[NQ * kb + qb]);
   }
@@ -150,7 +173,7 @@ __device__ __forceinline__ void soft_step(HalfS<NQ>& s, const float* nm, float s
 // finished half. Each MFMA is followed by its softmax step (a 16x16x32 MFMA of 16 cycles hides
 // about 8 cycles of vector work). Fragments LOOK slot pairs ahead are read from LDS. Scheduling
 // barriers keep the order.
-template <int U, int D, int NQ, int LOOK>
+template <int U, int D, int NQ, int LOOK, class L>
 __device__ __forceinline__ void pipe_slots(FwdState<D, NQ>& st, HalfS<NQ>& s_cur, HalfS<NQ>& sn, bf16x8* kf, bf16x8* vf,
                                            const __bf16* kq, const __bf16* vp, const __bf16* kn, const __bf16* vn,
                                            const HalfP<NQ>& pv, const float* nm, float sl2, float* acc,
@@ -160,10 +183,10 @@ __device__ __forceinline__ void pipe_slots(FwdState<D, NQ>& st, HalfS<NQ>& s_cur
     constexpr int I = U / (2 * NQ), qb = U % NQ;
     if constexpr (U % (2 * NQ) < NQ) {
       constexpr int kb = I / (D / 32), c = I % (D / 32);
-      if constexpr (qb == 0) kf[I + LOOK] = I + LOOK < NC ? k_frag<D>(kq, I + LOOK) : k_frag<D>(kn, I + LOOK - NC);
+      if constexpr (qb == 0) kf[I + LOOK] = I + LOOK < NC ? k_frag<D, L>(kq, I + LOOK) : k_frag<D, L>(kn, I + LOOK - NC);
       sn.b[NQ * kb + qb] = mfma16(kf[I], st.qf[qb][c], c == 0 ? floatx4{} : sn.b[NQ * kb + qb]);
     } else {
-      if constexpr (qb == 0) vf[I + LOOK] = I + LOOK < NC ? v_frag<D>(vp, I + LOOK) : v_frag<D>(vn, I + LOOK - NC);
+      if constexpr (qb == 0) vf[I + LOOK] = I + LOOK < NC ? v_frag<D, L>(vp, I + LOOK) : v_frag<D, L>(vn, I + LOOK - NC);
       st.o[qb][I] = mfma16(vf[I], pv.p[qb], st.o[qb][I]);
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -175,7 +198,7 @@ __device__ __forceinline__ void pipe_slots(FwdState<D, NQ>& st, HalfS<NQ>& s_cur
       soft_step<2 * U + 1>(s_cur, nm, sl2, acc, out);
     }
     __builtin_amdgcn_sched_barrier(0);
-    pipe_slots<U + 1, D, NQ, LOOK>(st, s_cur, sn, kf, vf, kq, vp, kn, vn, pv, nm, sl2, acc, out);
+    pipe_slots<U + 1, D, NQ, LOOK, L>(st, s_cur, sn, kf, vf, kq, vp, kn, vn, pv, nm, sl2, acc, out);
   }
 }
 
@@ -183,7 +206,7 @@ __device__ __forceinline__ void pipe_slots(FwdState<D, NQ>& st, HalfS<NQ>& s_cur
 // s_next) and O^T += V^T P^T of a finished half (V rows at vp, P in pv); after each group of
 // MFMAs one slice of the softmax of the current half (s_cur, whose K rows are at kc) is issued.
 // Returns P of the current half. Slot order is fixed with scheduling barriers.
-template <int D, int NQ>
+template <int D, int NQ, class L = PaddedRows>
 __device__ __forceinline__ HalfP<NQ> pipe_block(FwdState<D, NQ>& st, HalfS<NQ>& s_cur, const __bf16* kc,
                                                 HalfS<NQ>& s_next, const __bf16* kq, const __bf16* vp,
                                                 const __bf16* kn, const __bf16* vn, Ahead& ah, const HalfP<NQ>& pv,
@@ -207,7 +230,7 @@ __device__ __forceinline__ HalfP<NQ> pipe_block(FwdState<D, NQ>& st, HalfS<NQ>& 
   soft_fma<0>(s_cur, nm, sl2);
   soft_fma<1>(s_cur, nm, sl2);
   soft_exp<0>(s_cur);
-  pipe_slots<0, D, NQ, kLook>(st, s_cur, sn, kf, vf, kq, vp, kn, vn, pv, nm, sl2, acc, out);
+  pipe_slots<0, D, NQ, kLook, L>(st, s_cur, sn, kf, vf, kq, vp, kn, vn, pv, nm, sl2, acc, out);
   s_next = sn;
 #pragma unroll
   for (int i = 0; i < kLook; ++i) {
@@ -222,7 +245,7 @@ __device__ __forceinline__ HalfP<NQ> pipe_block(FwdState<D, NQ>& st, HalfS<NQ>& 
     ok = ok && acc[qb] <= kBigSum;
   }
   if (__builtin_expect(__builtin_amdgcn_ballot_w64(!ok) != 0, 0)) {
-    s_cur = scores32<D, NQ>(st, kc);
+    s_cur = scores32<D, NQ, L>(st, kc);
     rescale_half<D, NQ>(st, s_cur, sl2, acc);
     out = pack_half<NQ>(s_cur);
   }
@@ -232,11 +255,11 @@ __device__ __forceinline__ HalfP<NQ> pipe_block(FwdState<D, NQ>& st, HalfS<NQ>& 
 }
 
 // O^T += V^T P^T for one half, plain.
-template <int D, int NQ>
+template <int D, int NQ, class L = PaddedRows>
 __device__ __forceinline__ void pv_half(FwdState<D, NQ>& st, const __bf16* vt, const HalfP<NQ>& h) {
 #pragma unroll
   for (int db = 0; db < D / 16; ++db) {
-    const bf16x8 v = v_frag<D>(vt, db);
+    const bf16x8 v = v_frag<D, L>(vt, db);
 #pragma unroll
     for (int qb = 0; qb < NQ; ++qb) st.o[qb][db] = mfma16(v, h.p[qb], st.o[qb][db]);
   }

@@ -152,15 +152,15 @@ sra_status check_cache(const sra_paged_cache* c, bool pointers, bool tensors, Pa
   return SRA_OK;
 }
 
-// 16-row blocks per group of rows: as many as a sequence's (token, head of the group) rows fill on average. More would
+// Rows per group of rows: as many as a sequence's (token, head of the group) rows fill on average. More would
 // leave the matrix instructions' columns empty, fewer read K and V once for each of several groups.
-int tree_blocks(const sra_paged_cache& c, int32_t heads) {
+int tree_rows(const sra_paged_cache& c, int32_t heads) {
   const int64_t rows = (int64_t(c.tokens) + c.batch - 1) / c.batch * (heads / c.num_kv_heads);
-  return rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+  return rows <= 16 ? 16 : rows <= 32 ? 32 : kTreeShared;
 }
 
-size_t tree_slots_bytes(int nq, int32_t head_dim) {
-  return align_up(size_t(2) * kTreeGroups * 16 * nq * (head_dim + 2) * 4);
+size_t tree_slots_bytes(int rows, int32_t head_dim) {
+  return align_up(size_t(2) * kTreeGroups * rows * (head_dim + 2) * 4);
 }
 
 sra_status check_tree(const sra_paged_cache* c, int32_t num_heads, bool pointers, PagedCache* out, size_t* bytes) {
@@ -168,13 +168,15 @@ sra_status check_tree(const sra_paged_cache* c, int32_t num_heads, bool pointers
   if (st != SRA_OK) return st;
   if ((st = check_heads(num_heads, c->num_kv_heads, c->head_dim)) != SRA_OK) return st;
   if (int64_t(c->tokens) * num_heads > kMaxInt) return fail(SRA_ERR_UNSUPPORTED, "heads * tokens must be below 2^31");
-  const int nq = tree_blocks(*c, num_heads);
+  if (num_heads / c->num_kv_heads > kTreeMaxGroup)
+    return fail(SRA_ERR_UNSUPPORTED, "at most " + std::to_string(kTreeMaxGroup) + " query heads per K/V head");
+  const int rows = tree_rows(*c, num_heads);
   // the launch's chunks are counted in 32 bits
-  const int64_t keys = int64_t(c->max_pages) * c->page_size / kTreeChunk + c->tokens / kTreeChunk + 2;
-  const int64_t groups = c->batch + int64_t(c->tokens) * (num_heads / c->num_kv_heads) / (16 * nq);
+  const int64_t keys = int64_t(c->max_pages) * c->page_size / kTreeChunk + c->tokens / kTreeChunk + 2 + kTreeStart;
+  const int64_t groups = c->batch + int64_t(c->tokens) * (num_heads / c->num_kv_heads) / rows;
   if (double(keys) * double(groups) * c->num_kv_heads > double(kMaxInt))
     return fail(SRA_ERR_UNSUPPORTED, "the tokens times the cache's reach are too many for one call");
-  *bytes = tree_slots_bytes(nq, c->head_dim) + align_up(kTreeGroups * sizeof(TreeSplit));
+  *bytes = tree_slots_bytes(rows, c->head_dim) + align_up(kTreeGroups * sizeof(TreeSplit));
   return SRA_OK;
 }
 
@@ -388,7 +390,7 @@ sra_status sra_tree_attention(const sra_paged_cache* c, int32_t num_heads, const
   if (misaligned(tree, 8)) return fail(SRA_ERR_INVALID_ARGUMENT, "tree must be 8-byte aligned");
   if ((st = check_workspace(workspace, workspace_bytes, need)) != SRA_OK) return st;
   hipStream_t s = static_cast<hipStream_t>(stream);
-  const int nq = tree_blocks(*c, num_heads);
+  const int rows = tree_rows(*c, num_heads);
   a.q = static_cast<const __bf16*>(q);
   a.k = static_cast<const __bf16*>(k);
   a.v = static_cast<const __bf16*>(v);
@@ -399,10 +401,12 @@ sra_status sra_tree_attention(const sra_paged_cache* c, int32_t num_heads, const
   a.o = static_cast<__bf16*>(o);
   a.lse = lse;
   a.heads = num_heads;
+  const uint32_t G = uint32_t(num_heads / c->num_kv_heads);
+  a.group_magic = G > 1 ? uint32_t((uint64_t(1) << 32) / G + 1) : 0;
   a.scale_log2 = float(double(scale_of(softmax_scale, c->head_dim)) * 1.4426950408889634);
   a.part = static_cast<float*>(workspace);
-  a.split = reinterpret_cast<TreeSplit*>(static_cast<char*>(workspace) + tree_slots_bytes(nq, c->head_dim));
-  const hipError_t e = timed_launch(SRA_KERNEL_TREE, s, [&] { return launch_tree(a, nq, c->head_dim, s); });
+  a.split = reinterpret_cast<TreeSplit*>(static_cast<char*>(workspace) + tree_slots_bytes(rows, c->head_dim));
+  const hipError_t e = timed_launch(SRA_KERNEL_TREE, s, [&] { return launch_tree(a, rows, c->head_dim, s); });
   return e == hipSuccess ? SRA_OK : hip_fail(e, "tree attention launch");
 }
 

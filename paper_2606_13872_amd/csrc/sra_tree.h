@@ -12,6 +12,7 @@ constexpr int kTreeGroups = 256;     // workgroups of a launch: one per compute 
 // waves are a chain of latencies (about 5 us, the time of as many chunks of four waves when the cache bounds them).
 constexpr int kTreeStart = 8;
 constexpr int kTreeMinRun = kTreeStart + 8;  // a workgroup takes at least so much: two chunks per wave
+constexpr int kTreeMaxGroup = 1024;          // query heads of a K/V head
 
 #ifndef SRA_HD
 #ifdef __HIPCC__
@@ -68,8 +69,9 @@ struct TreeArgs {
   __bf16* o;                // dense
   float* lse;               // [heads, tokens]
   int32_t heads;
+  uint32_t group_magic;     // ceil(2^32 / G), for exact divisions of small numbers by G = heads / kv_heads > 1
   float scale_log2;
-  float* part;              // [2 kTreeGroups] slots: O [16 NQ, D], then (m, l) per row
+  float* part;              // [2 kTreeGroups] slots: O [rows, D], then (m, l) per row (rows per group of rows)
   TreeSplit* split;         // [kTreeGroups]
 };
 
@@ -82,8 +84,9 @@ struct AppendArgs {
   int32_t row_elems;        // kv_heads * D
 };
 
-// nq: 16-row blocks per group of rows (1, 2 or 4)
-hipError_t launch_tree(const TreeArgs& a, int nq, int head_dim, hipStream_t stream);
+// rows per group of rows: 16 or 32 (each wave takes its own keys) or kTreeShared (each wave its own rows)
+constexpr int kTreeShared = 256;
+hipError_t launch_tree(const TreeArgs& a, int rows, int head_dim, hipStream_t stream);
 hipError_t launch_append(const AppendArgs& a, hipStream_t stream);
 
 }  // namespace sra

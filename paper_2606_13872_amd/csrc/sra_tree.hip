@@ -13,15 +13,15 @@
 // In a workgroup each of the four waves takes every fourth chunk, alone: it loads the chunk's K and V rows into an
 // LDS ring of its own (global -> LDS, the chunks behind it in flight, no barrier), computes S^T = K Q^T, the running maximum and
 // sum, and O^T += V^T P^T on 16x16x32 MFMAs; at the end of a run the waves' results are merged through LDS.
-#include "sra_tiles.h"
+#include "sra_fwd_pipe.h"
 #include "sra_tree.h"
 
 namespace sra {
 
 namespace {
-constexpr float kLn2 = 0.69314718055994530942f;
 constexpr int kTreeWaves = 4;
 constexpr int kTreeThreads = kTreeWaves * 64;
+constexpr int kSharedChunk = 64;
 template <int D> constexpr int kStages = D == 128 ? 2 : 4;  // chunks of a wave's ring: 32 KB
 typedef const __attribute__((address_space(4))) int32_t* const_ints;  // read by scalar loads
 }  // namespace
@@ -31,80 +31,158 @@ __device__ __forceinline__ void wait_vmem_to() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
+// Inclusive scans over the lanes of a wave (DPP: rows of 16, then their last lanes to the rows behind).
+template <int kCtrl, int kRows>
+__device__ __forceinline__ int dpp_move(int x, int none) {
+  return __builtin_amdgcn_update_dpp(none, x, kCtrl, kRows, 0xf, false);
+}
+template <class F>
+__device__ __forceinline__ int wave_scan(int x, int none, F f) {
+  x = f(x, dpp_move<0x111, 0xf>(x, none));  // row_shr 1, 2, 4, 8
+  x = f(x, dpp_move<0x112, 0xf>(x, none));
+  x = f(x, dpp_move<0x114, 0xf>(x, none));
+  x = f(x, dpp_move<0x118, 0xf>(x, none));
+  x = f(x, dpp_move<0x142, 0xa>(x, none));  // lane 15 to row 1, lane 47 to row 3
+  return f(x, dpp_move<0x143, 0xc>(x, none));  // lane 31 to rows 2 and 3
+}
+
 // Bounds of the sequences: first[b] .. first[b + 1] are b's tokens (cu_tokens clamped into [0, tokens] and never
-// falling, so no token has two sequences), chunk[b] .. chunk[b + 1] the costs, in chunks, of its groups of rows of all
-// K/V heads.
+// falling, so no token has two sequences), ctx[b] its cached positions, cost[b] .. cost[b + 1] the costs, in chunks, of
+// its groups of rows of all K/V heads.
 struct TreeBounds {
   int32_t first[kTreeMaxBatch + 1];
-  int32_t chunk[kTreeMaxBatch + 1];
-  int32_t wave[2][kTreeWaves];
+  int32_t cost[kTreeMaxBatch + 1];
+  int32_t ctx[kTreeMaxBatch];
 };
 
-template <int NQ>
+__device__ __forceinline__ int group_div(const TreeArgs& a, int G, int x) {  // x / G, x < G + 256
+  return G == 1 ? x : int(__umulhi(uint32_t(x), a.group_magic));
+}
+
+// Every wave fills all of s, with the same values, so none waits for another. R rows to a group, C keys to a chunk.
+template <int R, int C>
 __device__ __forceinline__ void tree_bounds(const TreeArgs& a, TreeBounds& s) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = a.c.batch;
+  const int lane = threadIdx.x & 63, n = a.c.batch;
   const int G = a.heads / a.c.kv_heads;
-  int carry_first = 0, carry_chunk = 0;
-  if (threadIdx.x == 0) s.chunk[0] = 0;
-  for (int b0 = 0; b0 < n; b0 += kTreeThreads) {
-    const int b = b0 + threadIdx.x;
-    const bool in = b < n;
+  int carry_first = 0, carry_cost = 0;
+  if (lane == 0) s.cost[0] = 0;
+  int f = 0, end = 0, ctx = 0;
+  auto read = [&](int b) {
+    f = end = ctx = 0;
+    if (b < n) {
+      f = a.c.cu_tokens[b];
+      end = a.c.cu_tokens[b + 1];
+      ctx = cache_context(a.c, b);
+    }
+  };
+  read(lane);
+  for (int b0 = 0; b0 < n; b0 += 64) {
+    const int b = b0 + lane;
     // first tokens: the running maximum of the clamped cu_tokens[b]
-    int f = in ? min(max(a.c.cu_tokens[b], 0), a.c.tokens) : 0;
-    const int end_raw = in ? min(max(a.c.cu_tokens[b + 1], 0), a.c.tokens) : 0;
-    const int ctx = in ? cache_context(a.c, b) : 0;
-#pragma unroll
-    for (int w = 1; w < 64; w <<= 1) {
-      const int y = __shfl_up(f, w, 64);
-      if (lane >= w) f = max(f, y);
+    int first = min(max(f, 0), a.c.tokens);
+    const int last = min(max(end, 0), a.c.tokens), cached = ctx;
+    read(b + 64);  // the next ones, on their way during the scans
+    first = max(carry_first, wave_scan(first, 0, [](int x, int y) { return max(x, y); }));
+    const int t = max(first, last) - first;
+    const int chunks = kTreeStart + (cached + t + C - 1) / C;
+    int x = b < n && t > 0 ? chunks * ((t * G + R - 1) / R) * a.c.kv_heads : 0;
+    x = carry_cost + wave_scan(x, 0, [](int x, int y) { return x + y; });
+    if (b < n) {
+      s.first[b] = first;
+      s.ctx[b] = cached;
+      s.cost[b + 1] = x;
+      if (b == n - 1) s.first[n] = first + t;
     }
-    if (lane == 63) s.wave[0][wave] = f;
-    __syncthreads();
-    f = max(f, carry_first);
-    for (int w = 0; w < wave; ++w) f = max(f, s.wave[0][w]);
-    const int end = max(f, end_raw), t = end - f;
-    const int chunks = kTreeStart + (ctx + t + kTreeChunk - 1) / kTreeChunk;
-    int x = t > 0 ? chunks * ((t * G + 16 * NQ - 1) / (16 * NQ)) * a.c.kv_heads : 0;
-#pragma unroll
-    for (int w = 1; w < 64; w <<= 1) {
-      const int y = __shfl_up(x, w, 64);
-      if (lane >= w) x += y;
-    }
-    if (lane == 63) s.wave[1][wave] = x;
-    __syncthreads();
-    x += carry_chunk;
-    for (int w = 0; w < wave; ++w) x += s.wave[1][w];
-    if (in) {
-      s.first[b] = f;
-      s.chunk[b + 1] = x;
-      if (b == n - 1) s.first[n] = end;
-    }
-    for (int w = 0; w < kTreeWaves; ++w) {
-      carry_first = max(carry_first, s.wave[0][w]);
-      carry_chunk += s.wave[1][w];
-    }
-    __syncthreads();
+    carry_first = __builtin_amdgcn_readlane(first, 63);
+    carry_cost = __builtin_amdgcn_readlane(x, 63);
   }
-  __syncthreads();
+}
+
+// The sequence that cost position x belongs to: the first b with cost[b + 1] > x. Two looks of 64 lanes.
+__device__ __forceinline__ int tree_sequence(const TreeBounds& s, int n, int x) {
+  const int lane = threadIdx.x & 63, step = (n + 63) >> 6;
+  auto look = [&](int b, int by, bool in) {  // how many of cost[b + by], cost[b + 2 by], .. (b + 64 by at most) x is past
+    const int e = b + (lane + 1) * by;
+    return __builtin_popcountll(__builtin_amdgcn_ballot_w64(in && e <= n && s.cost[min(e, n)] <= x));
+  };
+  const int b = step * look(0, step, true);
+  return step == 1 ? b : b + look(b, 1, lane < step);
+}
+
+// One run's share of one group of rows.
+struct TreeSegment {
+  int b, t0, t, ctx;   // sequence, first token, tokens, cached positions
+  int kvh, row0, rows;
+  int n, c0, c1;       // chunks of the group, and of this run
+  int origin;          // cost position of the group's first chunk
+};
+template <int R, int C>
+__device__ __forceinline__ TreeSegment tree_segment(const TreeArgs& a, const TreeBounds& s, int G, int x, int end) {
+  TreeSegment g;
+  g.b = __builtin_amdgcn_readfirstlane(tree_sequence(s, a.c.batch, x));
+  g.t0 = __builtin_amdgcn_readfirstlane(s.first[g.b]);
+  g.t = __builtin_amdgcn_readfirstlane(s.first[g.b + 1]) - g.t0;
+  g.ctx = __builtin_amdgcn_readfirstlane(s.ctx[g.b]);
+  g.n = (g.ctx + g.t + C - 1) / C;  // keys: the context's, then the new tokens'
+  const int blocks = (g.t * G + R - 1) / R, cost = kTreeStart + g.n;
+  const int u = x - __builtin_amdgcn_readfirstlane(s.cost[g.b]), grp = u / cost;
+  g.origin = x - (u - grp * cost) + kTreeStart;
+  g.c0 = max(x - g.origin, 0);
+  g.c1 = min(g.n, end - g.origin);
+  g.kvh = blocks == 1 ? grp : grp / blocks;
+  g.row0 = (grp - g.kvh * blocks) * R;
+  g.rows = min(R, g.t * G - g.row0);
+  return g;
+}
+
+// Which of the new tokens a row sees, by chunk: bit e of the word is position p0 + e; `to` = cached positions behind p0.
+__device__ __forceinline__ uint32_t tree_word(bool has_tree, uint64_t tree, int tok, int to) {
+  uint32_t draft;
+  if (has_tree) {
+    draft = to >= 32 ? 0 : to >= 0 ? uint32_t(tree << to) : to > -64 ? uint32_t(tree >> -to) : 0;
+  } else {
+    const int last = tok + to;  // a chain: up to the token itself
+    draft = last >= 31 ? ~0u : last < 0 ? 0 : (2u << last) - 1;
+  }
+  return draft | (to >= 32 ? ~0u : to > 0 ? (1u << to) - 1 : 0);
+}
+
+// A lane's key as a row to load: the cache's, a new token's, or, for one that does not exist, the sequence's first new
+// token (a row that is there).
+struct TreeKey {
+  uint64_t k, v;
+  bool exists;
+};
+__device__ __forceinline__ TreeKey tree_key(const TreeArgs& a, const TreeSegment& g, int head_dim, int pos) {
+  const PagedCache& c = a.c;
+  TreeKey r;
+  const int page = pos < g.ctx ? cache_page(c, g.b, pos) : -1;
+  r.exists = page >= 0 || (pos >= g.ctx && pos - g.ctx < g.t);
+  const __bf16 *k, *v;
+  if (page >= 0) {
+    const int64_t slot = pos & ((1 << c.page_shift) - 1);
+    k = c.k + page * c.k_page + slot * c.k_token;
+    v = c.v + page * c.v_page + slot * c.v_token;
+  } else {
+    const int64_t fresh = g.t0 + (pos < g.ctx ? 0 : min(pos - g.ctx, g.t - 1));
+    k = a.k + fresh * a.ks;
+    v = a.v + fresh * a.vs;
+  }
+  r.k = reinterpret_cast<uint64_t>(k + int64_t(g.kvh) * head_dim);
+  r.v = reinterpret_cast<uint64_t>(v + int64_t(g.kvh) * head_dim);
+  return r;
+}
+__device__ __forceinline__ uint64_t lane_u64(uint64_t x, int lane) {
+  const uint32_t lo = __shfl(int(uint32_t(x)), lane, 64), hi = __shfl(int(uint32_t(x >> 32)), lane, 64);
+  return (uint64_t(hi) << 32) | lo;
 }
 
 // Per-wave state of a run over one group of rows.
 template <int D, int NQ>
 struct TreeState {
-  static constexpr bool kAgpr = NQ == 4;  // O in AGPRs (inline-assembly MFMAs): with it the VGPRs would not do
   bf16x8 qf[NQ][D / 32];  // Q^T B fragments (lane = row)
   floatx4 o[NQ][D / 16];
   float m[NQ], l[NQ];     // running maximum (log2 units), this lane's part of the sum
-  // O may be read and written by vector instructions from here on
-  __device__ __forceinline__ void settle() {
-    if constexpr (kAgpr) {
-      mfma_drain();
-#pragma unroll
-      for (int qb = 0; qb < NQ; ++qb)
-#pragma unroll
-        for (int db = 0; db < D / 16; ++db) asm volatile("" : "+a"(o[qb][db]));
-    }
-  }
 };
 
 // P of a chunk against the running maxima m as they are, and the lane's partial sums; false where one is above
@@ -136,18 +214,26 @@ __device__ __forceinline__ bool tree_soft(const TreeState<D, NQ>& st, const floa
 template <int D, int NQ>
 __device__ __forceinline__ void tree_rescale(TreeState<D, NQ>& st, const floatx4 (&s)[2][NQ], bf16x8 (&p)[NQ],
                                              float (&sum)[NQ], float sl2) {
-  st.settle();
+  float alpha[NQ];
+  bool scale = false;  // some row has an O to scale (at a run's first chunk none has)
 #pragma unroll
   for (int qb = 0; qb < NQ; ++qb) {
     const floatx4 x = s[0][qb], y = s[1][qb];
     const float mx = quad_max(max2f(max3f(x[0], x[1], max2f(x[2], x[3])), max3f(y[0], y[1], max2f(y[2], y[3])))) * sl2;
-    if (mx > st.m[qb]) {
-      const float alpha = fast_exp2(st.m[qb] - mx);  // 0 when m was -inf
-      st.m[qb] = mx;
-      st.l[qb] *= alpha;
+    const bool up = mx > st.m[qb];
+    scale |= up && st.m[qb] != -INFINITY;
+    alpha[qb] = up ? st.m[qb] == -INFINITY ? 0.f : fast_exp2(st.m[qb] - mx) : 1.f;
+    st.m[qb] = up ? mx : st.m[qb];
+    st.l[qb] *= alpha[qb];
+  }
+  if (__builtin_amdgcn_ballot_w64(scale)) {
 #pragma unroll
-      for (int db = 0; db < D / 16; ++db) st.o[qb][db] *= alpha;
-    }
+    for (int qb = 0; qb < NQ; ++qb)
+#pragma unroll
+      for (int db = 0; db < D / 16; ++db) st.o[qb][db] *= alpha[qb];
+  }
+#pragma unroll
+  for (int qb = 0; qb < NQ; ++qb) {
     const float nm = st.m[qb] == -INFINITY ? 0.f : -st.m[qb];  // a row that has seen nothing keeps P = 0
     float acc = 0.f;
 #pragma unroll
@@ -175,6 +261,7 @@ __device__ __forceinline__ void tree_chunk(TreeState<D, NQ>& st, uint32_t kt, ui
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       const bf16x8 k = lds_ld8(((kt + row) ^ (64 * c)) + kb * 32 * D);
+      if (c == 0) __builtin_amdgcn_sched_barrier(0);  // all fragments at once would not fit the VGPRs
 #pragma unroll
       for (int qb = 0; qb < NQ; ++qb) s[kb][qb] = mfma16(k, st.qf[qb][c], c == 0 ? floatx4{} : s[kb][qb]);
     }
@@ -201,12 +288,10 @@ __device__ __forceinline__ void tree_chunk(TreeState<D, NQ>& st, uint32_t kt, ui
 #pragma unroll
   for (int db = 0; db < ND; ++db) {
     const uint32_t x = (vt + tr) ^ (32 * db);
+    if (db % 4 == 0) __builtin_amdgcn_sched_barrier(0);
     const bf16x8 v = cat8(lds_ld_tr(x), lds_ld_tr(x + 32 * D));
 #pragma unroll
-    for (int qb = 0; qb < NQ; ++qb) {
-      if constexpr (TreeState<D, NQ>::kAgpr) mfma16_agpr(st.o[qb][db], v, p[qb]);
-      else st.o[qb][db] = mfma16(v, p[qb], st.o[qb][db]);
-    }
+    for (int qb = 0; qb < NQ; ++qb) st.o[qb][db] = mfma16(v, p[qb], st.o[qb][db]);
   }
 }
 
@@ -228,8 +313,8 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
   constexpr int per_xcd = kTreeGroups / kNumXcd;
   const int w = __builtin_amdgcn_readfirstlane((blockIdx.x % kNumXcd) * per_xcd + blockIdx.x / kNumXcd);
 
-  tree_bounds<NQ>(a, bounds);
-  const int total = __builtin_amdgcn_readfirstlane(bounds.chunk[c.batch]);
+  tree_bounds<R, kTreeChunk>(a, bounds);
+  const int total = __builtin_amdgcn_readfirstlane(bounds.cost[c.batch]);
   const int run = max(kTreeMinRun, (total + kTreeGroups - 1) / kTreeGroups);
   const int begin = int(min(int64_t(w) * run, int64_t(total))), end = int(min(int64_t(begin) + run, int64_t(total)));
   TreeSplit split{0, 0, 0, 0, 0};
@@ -244,25 +329,11 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
   for (int i = 0; i < kKinds; ++i) chunk16[i] = ((lane % CPR) ^ swz<D>(i * RPI + lrow)) * 8;
 
   for (int x = begin; x < end;) {
-    // the sequence that chunk x belongs to
-    int b = 0;
-    for (int lo = 0, hi = c.batch; lo < hi;) {  // the last b with chunk[b] <= x and chunks of its own
-      b = (lo + hi) >> 1;
-      if (__builtin_amdgcn_readfirstlane(bounds.chunk[b + 1]) <= x) lo = ++b;
-      else hi = b;
-    }
-    const int t0 = __builtin_amdgcn_readfirstlane(bounds.first[b]);
-    const int t = __builtin_amdgcn_readfirstlane(bounds.first[b + 1]) - t0;
-    const int ctx = __builtin_amdgcn_readfirstlane(cache_context(c, b));
-    const int n = (ctx + t + kTreeChunk - 1) / kTreeChunk;  // keys: the context's, then the new tokens'
-    const int blocks = (t * G + R - 1) / R;
-    const int u = x - __builtin_amdgcn_readfirstlane(bounds.chunk[b]), cost = kTreeStart + n, grp = u / cost;
-    // chunk i of the group is at origin + i
-    const int origin = x - (u - grp * cost) + kTreeStart, c0 = max(x - origin, 0), c1 = min(n, end - origin);
-    x = origin + n;
-    if (c0 >= c1) continue;  // the run ends before its first chunk
-    const int kvh = grp / blocks, row0 = (grp - kvh * blocks) * R, rows = min(R, t * G - row0);
-    const const_ints table = (const_ints)(uintptr_t)(c.table + int64_t(b) * c.table_stride);
+    const TreeSegment seg = tree_segment<R, kTreeChunk>(a, bounds, G, x, end);
+    const int t0 = seg.t0, ctx = seg.ctx, n = seg.n, c0 = seg.c0, c1 = seg.c1;
+    x = seg.origin + n;
+    if (c0 >= c1) continue;  // the run ends before the group's first chunk
+    const const_ints table = (const_ints)(uintptr_t)(c.table + int64_t(seg.b) * c.table_stride);
 
     // Page ids of chunk i's four groups of 8 rows (a page holds a multiple of 8), where the chunk is all context.
     struct Ids {
@@ -288,7 +359,7 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
           constexpr int kPer = kInstr / 4;  // load instructions of 8 rows
 #pragma unroll
           for (int kv = 0; kv < 2; ++kv) {
-            const __bf16* base = (kv ? c.v : c.k) + int64_t(kvh) * D;
+            const __bf16* base = (kv ? c.v : c.k) + int64_t(seg.kvh) * D;
             const int64_t ps = kv ? c.v_page : c.k_page, ts = kv ? c.v_token : c.k_token;
             const uint32_t lane_row = uint32_t(lrow * ts);
 #pragma unroll
@@ -302,22 +373,19 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
           return ~0u;
         }
       }
-      // the context's end, new tokens, or a page that is none: row by row. Keys that do not exist read a new token of
-      // the sequence instead, a row that is there
-      const int pos = p0 + (lane & 31);
-      const int page = pos < ctx ? cache_page(c, b, pos) : -1;
-      const uint32_t exist = uint32_t(__builtin_amdgcn_ballot_w64(page >= 0 || (pos >= ctx && pos - ctx < t)));
+      // the context's end, new tokens, or a page that is none: row by row
+      const TreeKey key = tree_key(a, seg, D, p0 + (lane & 31));
 #pragma unroll 1
-      for (int e = 0; e < 2 * kInstr; ++e) {  // K, then V: the waits below count on that order
-        const int j = e % kInstr, r = j * RPI + lrow, p = p0 + r;
-        const bool is_v = e >= kInstr;
-        const int64_t id = __shfl(page, r, 64), slot = p & (page_rows - 1);
-        const int64_t fresh = t0 + (p < ctx ? 0 : min(p - ctx, t - 1));
-        const __bf16* src = id >= 0 ? (is_v ? c.v : c.k) + id * (is_v ? c.v_page : c.k_page) + slot * (is_v ? c.v_token : c.k_token)
-                                    : (is_v ? a.v : a.k) + fresh * (is_v ? a.vs : a.ks);
-        lds_dma_x4_at(src + kvh * D + ((lane % CPR) ^ swz<D>(r)) * 8, la + is_v * kTile + j * 1024);
+      for (int kv = 0; kv < 2; ++kv) {  // K, then V: the waits below count on that order
+        const uint64_t mine = kv ? key.v : key.k;
+#pragma unroll 1
+        for (int j = 0; j < kInstr; j += kKinds)
+#pragma unroll
+          for (int e = 0; e < kKinds; ++e)
+            lds_dma_x4_at(reinterpret_cast<const __bf16*>(lane_u64(mine, (j + e) * RPI + lrow)) + chunk16[e],
+                          la + kv * kTile + (j + e) * 1024);
       }
-      return exist;
+      return uint32_t(__builtin_amdgcn_ballot_w64(key.exists));
     };
 
     // chunk i + kTreeWaves k sits in stage k % NS; NS - 1 chunks are in flight behind the one that is worked on
@@ -331,14 +399,15 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
     }
     Ids ids = page_ids(c0 + wave + kAhead);  // of the chunk that is loaded next
     TreeState<D, NQ> st;
-    uint64_t tree[NQ];  // which drafted tokens the lane's row sees (a chain: all up to itself; see below)
+    uint64_t tree[NQ];  // which drafted tokens the lane's row sees
     int tok[NQ];
+    const int tok0 = seg.row0 / G, rem0 = seg.row0 - tok0 * G;  // the group's first row
 #pragma unroll
     for (int qb = 0; qb < NQ; ++qb) {
-      const int r = row0 + min(16 * qb + l16, rows - 1), token = r / G, h = kvh * G + r - token * G;
-      tok[qb] = token;
-      tree[qb] = a.tree ? a.tree[t0 + token] : 0;
-      const __bf16* src = a.q + int64_t(t0 + token) * a.qs + int64_t(h) * D + g * 8;
+      const int r = rem0 + min(16 * qb + l16, seg.rows - 1), dt = group_div(a, G, r), h = seg.kvh * G + r - dt * G;
+      tok[qb] = tok0 + dt;
+      tree[qb] = a.tree ? a.tree[t0 + tok[qb]] : 0;
+      const __bf16* src = a.q + int64_t(t0 + tok[qb]) * a.qs + int64_t(h) * D + g * 8;
 #pragma unroll
       for (int i = 0; i < NC; ++i) st.qf[qb][i] = ld8(src + i * 32);
 #pragma unroll
@@ -376,19 +445,8 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
       } else {
         uint32_t vis[NQ];
 #pragma unroll
-        for (int qb = 0; qb < NQ; ++qb) {
-          // bit e is position 32 i + e, new token e - to
-          const int to = ctx - i * kTreeChunk;
-          uint32_t draft;
-          if (a.tree) {
-            draft = to >= 32 ? 0 : to >= 0 ? uint32_t(tree[qb] << to) : to > -64 ? uint32_t(tree[qb] >> -to) : 0;
-          } else {
-            const int last = tok[qb] + to;
-            draft = last >= 31 ? ~0u : last < 0 ? 0 : (2u << last) - 1;
-          }
-          const uint32_t cached = to >= 32 ? ~0u : to > 0 ? (1u << to) - 1 : 0;
-          vis[qb] = exist[0] & (cached | draft);
-        }
+        for (int qb = 0; qb < NQ; ++qb)
+          vis[qb] = exist[0] & tree_word(a.tree, tree[qb], tok[qb], ctx - i * kTreeChunk);
         tree_chunk<D, NQ, true>(st, kt, vt, row, tr, vis, sl2, land_v);
       }
 #pragma unroll
@@ -405,7 +463,6 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
         ml[wave][16 * qb + l16][1] = l;
       }
     }
-    st.settle();
     float* const mine = reinterpret_cast<float*>(lds + wave * kRing);
 #pragma unroll
     for (int qb = 0; qb < NQ; ++qb)
@@ -416,8 +473,11 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
     const bool whole = c0 == 0 && c1 == n;
     const int slot = 2 * w + (c0 == 0);
     float* const part = a.part + int64_t(slot) * R * (D + 2);
-    for (int e = threadIdx.x; e < rows * (D / 4); e += kTreeThreads) {
-      const int r = e / (D / 4), q = e % (D / 4);
+    constexpr int kRowStep = kTreeThreads / (D / 4);
+#pragma unroll 2
+    for (int r0 = 0; r0 < R; r0 += kRowStep) {
+      const int r = r0 + threadIdx.x / (D / 4), q = threadIdx.x % (D / 4);
+      if (r >= seg.rows) continue;
       float m = -INFINITY;
 #pragma unroll
       for (int i = 0; i < kTreeWaves; ++i) m = max2f(m, ml[i][r][0]);
@@ -431,30 +491,279 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
         o += f * *reinterpret_cast<const floatx4*>(reinterpret_cast<const float*>(lds + i * kRing) + r * D + (q ^ (r & 15)) * 4);
       }
       if (whole) {
-        const int rr = row0 + r, token = rr / G, h = kvh * G + rr - token * G;
+        const int rr = rem0 + r, dt = group_div(a, G, rr), h = seg.kvh * G + rr - dt * G;
+        const int64_t token = t0 + tok0 + dt;
         const float inv = l == 0.f ? 0.f : 1.f / l;
         bf16x4 y;
 #pragma unroll
         for (int i = 0; i < 4; ++i) y[i] = (__bf16)(o[i] * inv);
-        *reinterpret_cast<bf16x4*>(a.o + (int64_t(t0 + token) * a.heads + h) * D + 4 * q) = y;
-        if (q == 0) a.lse[int64_t(h) * c.tokens + t0 + token] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+        *reinterpret_cast<bf16x4*>(a.o + (token * a.heads + h) * D + 4 * q) = y;
+        if (q == 0) a.lse[int64_t(h) * c.tokens + token] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
       } else {
         *reinterpret_cast<floatx4*>(part + r * D + 4 * q) = o;
         if (q == 0) *reinterpret_cast<float2*>(part + R * D + 2 * r) = float2{m, l};
       }
     }
     if (!whole && c0 == 0)  // the group's first keys
-      split = TreeSplit{(origin + n - 1) / run - w + 1, t0, row0, rows, kvh};
+      split = TreeSplit{(seg.origin + n - 1) / run - w + 1, t0, seg.row0, seg.rows, seg.kvh};
     __syncthreads();  // the rings and ml are free again
   }
   if (threadIdx.x == 0) a.split[w] = split;
 }
 
-// Groups of rows that several workgroups share, from their pieces, in key order: with M the largest of their maxima,
-// O = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i. D / 4 threads per row.
+// A 32-key half whose keys p0 .. a row sees by the bits of vis[qb] (LDS rows past the last key hold a row that is there).
 template <int D, int NQ>
+__device__ __forceinline__ void tree_half(FwdState<D, NQ>& st, const __bf16* kt, const __bf16* vt, const uint32_t* vis,
+                                          float sl2) {
+  const int g = (threadIdx.x & 63) >> 4;
+  HalfS<NQ> s = scores32<D, NQ, SwizzledRows>(st, kt);
+#pragma unroll
+  for (int j = 0; j < 2 * NQ; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s.b[j][i] = (vis[j % NQ] >> (16 * (j / NQ) + 4 * g + i)) & 1 ? s.b[j][i] : -INFINITY;
+  float sum[NQ];
+  rescale_half<D, NQ>(st, s, sl2, sum);
+#pragma unroll
+  for (int qb = 0; qb < NQ; ++qb) st.l[qb] += sum[qb];
+  pv_half<D, NQ, SwizzledRows>(st, vt, pack_half<NQ>(s));
+}
+
+// The same for many rows (trees of drafted tokens): up to 256 rows to a group, so that K and V are read once for all of
+// them. Eight waves (two per SIMD) own 32 rows each; the keys go through LDS in 64-key tiles that all of them read.
+// Whole tiles of the context run through the software pipeline of sra_fwd_pipe.h (three buffers each for K and V, loads
+// two and one tiles ahead), the context's end and the new tokens behind them, masked. Where the table names a page
+// that is none, all of the group's tiles run masked.
+template <int D>
+__global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
+sra_tree_shared_kernel(TreeArgs a) {
+  constexpr int NQ = 2, NC = D / 32, ND = D / 16, R = kTreeShared, C = kSharedChunk;
+  using TL = SwzTile<D, C>;
+  constexpr int RPI = 512 / D, CPR = D / 8, kPer = TL::kInstr / kWaves;  // rows of a load instruction; a wave's of a tile
+  static_assert(R == kWaves * 16 * NQ && kPer >= 1 && RPI * kWaves % 8 == 0 && C == kFwdKeyStep, "tiles by waves");
+  __shared__ __attribute__((aligned(1024))) __bf16 kbuf0[TL::kElems];
+  __shared__ __attribute__((aligned(1024))) __bf16 kbuf1[TL::kElems];
+  __shared__ __attribute__((aligned(1024))) __bf16 kbuf2[TL::kElems];
+  __shared__ __attribute__((aligned(1024))) __bf16 vbuf0[TL::kElems];
+  __shared__ __attribute__((aligned(1024))) __bf16 vbuf1[TL::kElems];
+  __shared__ __attribute__((aligned(1024))) __bf16 vbuf2[TL::kElems];
+  __bf16* const kb[3] = {kbuf0, kbuf1, kbuf2};
+  __bf16* const vb[3] = {vbuf0, vbuf1, vbuf2};
+  __shared__ TreeBounds bounds;
+  const PagedCache& c = a.c;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 4, l16 = lane & 15;
+  const int G = a.heads / c.kv_heads, page_mask = (1 << c.page_shift) - 1;
+  const float sl2 = a.scale_log2;
+  constexpr int per_xcd = kTreeGroups / kNumXcd;
+  const int w = __builtin_amdgcn_readfirstlane((blockIdx.x % kNumXcd) * per_xcd + blockIdx.x / kNumXcd);
+
+  tree_bounds<R, C>(a, bounds);
+  const int total = __builtin_amdgcn_readfirstlane(bounds.cost[c.batch]);
+  const int run = max(kTreeMinRun, (total + kTreeGroups - 1) / kTreeGroups);
+  const int begin = int(min(int64_t(w) * run, int64_t(total))), end = int(min(int64_t(begin) + run, int64_t(total)));
+  TreeSplit split{0, 0, 0, 0, 0};
+  // load instructions wave + 8 j of a tile: rows RPI (wave + 8 j) + lane / CPR, one swizzle for all j
+  const int lrow = RPI * wave + lane / CPR, chunk16 = ((lane % CPR) ^ swz<D>(lrow)) * 8;
+  const uint32_t koff = (uint32_t((lane / CPR) * c.k_token) + chunk16) * 2, voff = (uint32_t((lane / CPR) * c.v_token) + chunk16) * 2;
+
+  for (int x = begin; x < end;) {
+    const TreeSegment seg = tree_segment<R, C>(a, bounds, G, x, end);
+    const int t0 = seg.t0, ctx = seg.ctx, n = seg.n, c0 = seg.c0, c1 = seg.c1;
+    x = seg.origin + n;
+    if (c0 >= c1) continue;  // the run ends before the group's first tile
+    const const_ints table = (const_ints)(uintptr_t)(c.table + int64_t(seg.b) * c.table_stride);
+    int T = max(0, min(c1, ctx / C) - c0);  // whole tiles of the context
+    bool bad = false;
+    if (T > 0)
+      for (int p = (c0 * C >> c.page_shift) + lane; p <= ((c0 + T) * C - 1) >> c.page_shift; p += 64)
+        bad |= uint32_t(c.table[int64_t(seg.b) * c.table_stride + p]) >= uint32_t(c.pages);
+    if (__builtin_amdgcn_ballot_w64(bad)) T = 0;
+
+    // page ids of this wave's load instructions of tile i (an instruction's rows lie in one 8-row part of a page)
+    struct Ids {
+      int v[kPer];
+    };
+    auto page_ids = [&](int i) __attribute__((always_inline)) {
+      Ids ids{};
+      if (i < c0 + T)
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) ids.v[j] = table[(i * C + RPI * (wave + j * kWaves)) >> c.page_shift];
+      return ids;
+    };
+    const uint64_t kbase = uniform_u64(reinterpret_cast<uint64_t>(c.k + int64_t(seg.kvh) * D));
+    const uint64_t vbase = uniform_u64(reinterpret_cast<uint64_t>(c.v + int64_t(seg.kvh) * D));
+    auto issue = [&](int i, const Ids& ids, bool is_v, const __bf16* dst) __attribute__((always_inline)) {
+      const uint32_t la = lds_addr(dst) + wave * 1024;
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) {
+        const int slot = (i * C + RPI * (wave + j * kWaves)) & page_mask;
+        const int64_t row = ids.v[j] * (is_v ? c.v_page : c.k_page) + slot * (is_v ? c.v_token : c.k_token);
+        lds_dma_x4_off(uniform_u64((is_v ? vbase : kbase) + uint64_t(row) * 2), is_v ? voff : koff, la + j * kWaves * 1024);
+      }
+    };
+    int next_k = c0, next_v = c0;
+    Ids ids_k = page_ids(c0), ids_v = ids_k;  // of the tiles that are loaded next
+    auto issue_k = [&](const __bf16* dst) __attribute__((always_inline)) {
+      issue(next_k, ids_k, false, dst);
+      ids_k = page_ids(++next_k);
+    };
+    auto issue_v = [&](const __bf16* dst) __attribute__((always_inline)) {
+      issue(next_v, ids_v, true, dst);
+      ids_v = page_ids(++next_v);
+    };
+    if (T > 0) {
+      issue_k(kbuf0);
+      issue_v(vbuf0);
+      if (T > 1) issue_k(kbuf1);
+    }
+
+    FwdState<D, NQ> st;
+    const int wrow = wave * 16 * NQ;
+    const bool active = wrow < seg.rows;
+    const int tok0 = seg.row0 / G, rem0 = seg.row0 - tok0 * G;
+    auto row_of = [&](int qb) { return rem0 + min(wrow + 16 * qb + l16, seg.rows - 1); };
+#pragma unroll
+    for (int qb = 0; qb < NQ; ++qb) {
+      const int r = row_of(qb), dt = group_div(a, G, r), h = seg.kvh * G + r - dt * G;
+      const __bf16* src = a.q + int64_t(t0 + tok0 + dt) * a.qs + int64_t(h) * D + g * 8;
+#pragma unroll
+      for (int i = 0; i < NC; ++i) st.qf[qb][i] = ld8(src + i * 32);
+#pragma unroll
+      for (int db = 0; db < ND; ++db) st.o[qb][db] = floatx4{};
+      st.m[qb] = -INFINITY;
+      st.l[qb] = 0.f;
+    }
+    // land them here, behind the first tiles, not at their first use inside the loop
+#pragma unroll
+    for (int qb = 0; qb < NQ; ++qb)
+#pragma unroll
+      for (int i = 0; i < NC; ++i) asm volatile("" : "+v"(st.qf[qb][i]));
+
+    // Tile t sits in K buffer t % 3 and V buffer t % 3 (tile -1 in V buffer 2). Iteration t reads K(t) (second half),
+    // K(t+1) (first half), V(t-1) (second half) and V(t) (first half), and loads K(t+2) and V(t+1).
+    if (T > 0) {
+      for (int e = threadIdx.x * 8; e < 32 * D; e += kWaves * 64 * 8)
+        *reinterpret_cast<bf16x8*>(vbuf2 + 32 * D + e) = bf16x8{};
+      wait_vmem();
+      __syncthreads();
+      HalfP<NQ> p_hi;
+#pragma unroll
+      for (int qb = 0; qb < NQ; ++qb) p_hi.p[qb] = bf16x8{};
+      HalfS<NQ> s_lo = {}, s_hi = {};
+      if (active) s_lo = scores32<D, NQ, SwizzledRows>(st, kbuf0);
+      Ahead ah;
+#pragma unroll
+      for (int i = 0; i < kLook; ++i) {
+        ah.k[i] = k_frag<D, SwizzledRows>(kbuf0 + 32 * D, i);
+        ah.v[i] = v_frag<D, SwizzledRows>(vbuf2 + 32 * D, i);
+      }
+      auto iteration = [&](int t, auto phase) {
+        constexpr int P = decltype(phase)::value;
+        __bf16* const k_t = kb[P];
+        __bf16* const k_t1 = kb[(P + 1) % 3];
+        __bf16* const v_tm1 = vb[(P + 2) % 3];
+        __bf16* const v_t = vb[P];
+        if (t + 1 < T) issue_v(vb[(P + 1) % 3]);
+        if (t + 2 < T) issue_k(kb[(P + 2) % 3]);
+        if (active) {
+          const HalfP<NQ> p_lo = pipe_block<D, NQ, SwizzledRows>(st, s_lo, k_t, s_hi, k_t + 32 * D, v_tm1 + 32 * D, k_t1,
+                                                                 v_t, ah, p_hi, sl2);
+          p_hi = pipe_block<D, NQ, SwizzledRows>(st, s_hi, k_t + 32 * D, s_lo, k_t1, v_t, k_t1 + 32 * D, v_t + 32 * D, ah,
+                                                 p_lo, sl2);
+        }
+        wait_vmem();
+        __syncthreads();
+      };
+      using P0 = std::integral_constant<int, 0>;
+      using P1 = std::integral_constant<int, 1>;
+      using P2 = std::integral_constant<int, 2>;
+      int t = 0;
+      for (; t + 3 <= T; t += 3) {
+        iteration(t, P0{});
+        iteration(t + 1, P1{});
+        iteration(t + 2, P2{});
+      }
+      if (t < T) iteration(t, P0{});
+      if (t + 1 < T) iteration(t + 1, P1{});
+      if (active) {
+        const int last = (T - 1) % 3;
+        if (last == 0) pv_half<D, NQ, SwizzledRows>(st, vbuf0 + 32 * D, p_hi);
+        else if (last == 1) pv_half<D, NQ, SwizzledRows>(st, vbuf1 + 32 * D, p_hi);
+        else pv_half<D, NQ, SwizzledRows>(st, vbuf2 + 32 * D, p_hi);
+      }
+    }
+
+    // the masked tiles
+    for (int i = c0 + T; i < c1; ++i) {
+      __syncthreads();  // every wave is done with the buffers
+      const TreeKey key = tree_key(a, seg, D, i * C + lane);
+      const uint64_t exist = __builtin_amdgcn_ballot_w64(key.exists);
+#pragma unroll 1
+      for (int j = 0; j < kPer; ++j) {
+        const int r = lrow + j * RPI * kWaves;
+        lds_dma_x4_at(reinterpret_cast<const __bf16*>(lane_u64(key.k, r)) + chunk16, lds_addr(kbuf0) + (wave + j * kWaves) * 1024);
+        lds_dma_x4_at(reinterpret_cast<const __bf16*>(lane_u64(key.v, r)) + chunk16, lds_addr(vbuf0) + (wave + j * kWaves) * 1024);
+      }
+      uint64_t tree[NQ];  // which new tokens the lane's row sees
+      int tok[NQ];
+#pragma unroll
+      for (int qb = 0; qb < NQ; ++qb) {
+        tok[qb] = tok0 + group_div(a, G, row_of(qb));
+        tree[qb] = a.tree ? a.tree[t0 + tok[qb]] : 0;
+      }
+      wait_vmem();
+      __syncthreads();
+      if (active)
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+          uint32_t vis[NQ];
+#pragma unroll
+          for (int qb = 0; qb < NQ; ++qb)
+            vis[qb] = uint32_t(exist >> (32 * half)) & tree_word(a.tree, tree[qb], tok[qb], ctx - i * C - 32 * half);
+          tree_half<D, NQ>(st, kbuf0 + half * 32 * D, vbuf0 + half * 32 * D, vis, sl2);
+        }
+    }
+
+    const bool whole = c0 == 0 && c1 == n;
+    float* const part = a.part + int64_t(2 * w + (c0 == 0)) * R * (D + 2);
+    if (active) {
+#pragma unroll
+      for (int qb = 0; qb < NQ; ++qb) {
+        const int r = wrow + 16 * qb + l16;
+        const float l = quad_sum(st.l[qb]);
+        if (r >= seg.rows) continue;
+        if (whole) {
+          const int rr = rem0 + r, dt = group_div(a, G, rr), h = seg.kvh * G + rr - dt * G;
+          const int64_t token = t0 + tok0 + dt;
+          const float inv = l == 0.f ? 0.f : 1.f / l;
+          __bf16* orow = a.o + (token * a.heads + h) * D + 4 * g;
+#pragma unroll
+          for (int db = 0; db < ND; ++db) {
+            bf16x4 y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = (__bf16)(st.o[qb][db][e] * inv);
+            *reinterpret_cast<bf16x4*>(orow + db * 16) = y;
+          }
+          if (g == 0) a.lse[int64_t(h) * c.tokens + token] = l == 0.f ? -INFINITY : (st.m[qb] + log2f(l)) * kLn2;
+        } else {
+#pragma unroll
+          for (int db = 0; db < ND; ++db) *reinterpret_cast<floatx4*>(part + r * D + db * 16 + 4 * g) = st.o[qb][db];
+          if (g == 0) *reinterpret_cast<float2*>(part + R * D + 2 * r) = float2{st.m[qb], l};
+        }
+      }
+    }
+    if (!whole && c0 == 0)  // the group's first keys
+      split = TreeSplit{(seg.origin + n - 1) / run - w + 1, t0, seg.row0, seg.rows, seg.kvh};
+    __syncthreads();  // the buffers are free again
+  }
+  if (threadIdx.x == 0) a.split[w] = split;
+}
+
+// Groups of rows that several workgroups share, from their pieces, in key order: with M the largest of their maxima,
+// O = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i. D / 4 threads per row, R rows to a slot.
+template <int D, int R>
 __global__ void __launch_bounds__(kTreeThreads) sra_tree_combine_kernel(TreeArgs a) {
-  constexpr int TPR = D / 4, RPB = kTreeThreads / TPR, R = 16 * NQ;
+  constexpr int TPR = D / 4, RPB = kTreeThreads / TPR;
   constexpr int64_t kSlot = int64_t(R) * (D + 2);
   const int w = blockIdx.x;
   const TreeSplit sp = a.split[w];
@@ -515,25 +824,27 @@ __global__ void __launch_bounds__(kTreeThreads) sra_append_kernel(AppendArgs a) 
   }
 }
 
-template <int D, int NQ>
-static void launch_tree_nq(const TreeArgs& a, hipStream_t stream) {
+template <int D, int R>
+static void launch_tree_rows(const TreeArgs& a, hipStream_t stream) {
   constexpr int RPB = kTreeThreads / (D / 4);
-  hipLaunchKernelGGL((sra_tree_kernel<D, NQ>), dim3(kTreeGroups), dim3(kTreeThreads), 0, stream, a);
-  hipLaunchKernelGGL((sra_tree_combine_kernel<D, NQ>), dim3(kTreeGroups, (16 * NQ + RPB - 1) / RPB), dim3(kTreeThreads), 0,
-                     stream, a);
+  if constexpr (R == kTreeShared)
+    hipLaunchKernelGGL(sra_tree_shared_kernel<D>, dim3(kTreeGroups), dim3(kWaves * 64), 0, stream, a);
+  else
+    hipLaunchKernelGGL((sra_tree_kernel<D, R / 16>), dim3(kTreeGroups), dim3(kTreeThreads), 0, stream, a);
+  hipLaunchKernelGGL((sra_tree_combine_kernel<D, R>), dim3(kTreeGroups, R / RPB), dim3(kTreeThreads), 0, stream, a);
 }
 
-hipError_t launch_tree(const TreeArgs& a, int nq, int head_dim, hipStream_t stream) {
+template <int D>
+static void launch_tree_dim(const TreeArgs& a, int rows, hipStream_t stream) {
+  if (rows == 16) launch_tree_rows<D, 16>(a, stream);
+  else if (rows == 32) launch_tree_rows<D, 32>(a, stream);
+  else launch_tree_rows<D, kTreeShared>(a, stream);
+}
+
+hipError_t launch_tree(const TreeArgs& a, int rows, int head_dim, hipStream_t stream) {
   if (a.c.tokens <= 0) return hipSuccess;
-  if (head_dim == 128) {
-    if (nq == 1) launch_tree_nq<128, 1>(a, stream);
-    else if (nq == 2) launch_tree_nq<128, 2>(a, stream);
-    else launch_tree_nq<128, 4>(a, stream);
-  } else {
-    if (nq == 1) launch_tree_nq<64, 1>(a, stream);
-    else if (nq == 2) launch_tree_nq<64, 2>(a, stream);
-    else launch_tree_nq<64, 4>(a, stream);
-  }
+  if (head_dim == 128) launch_tree_dim<128>(a, rows, stream);
+  else launch_tree_dim<64>(a, rows, stream);
   return hipGetLastError();
 }
 
