@@ -16,12 +16,13 @@ namespace sra {
 
 namespace {
 
-// Costs in steps of a forward item (64 keys x 256 rows). A dQ step computes three products to the
-// forward's two, a dK/dV step four; both run at one wave per SIMD.
-constexpr double kStepCost[3] = {1.0, 1.5, 2.0};
-constexpr double kItemCost = 2.5;      // an item's loads before the first product and its epilogue
-constexpr double kCombineCost = 3.5;   // the combine launch
-constexpr double kSlotCost[3] = {0.25, 0.25, 0.5};  // writing and reading the partial results of one piece
+// Costs in steps of a forward item (64 keys x 256 rows; 1.75 us at head_dim 128, measured, as the others are). A
+// dQ step computes three products to the forward's two, a dK/dV step four.
+constexpr double kStepCost[3] = {1.0, 1.5, 1.85};
+constexpr double kItemCost[3] = {2.9, 4.5, 6.0};  // an item's loads before the first product, diagonal and epilogue
+constexpr double kSlotCost[3] = {2.2, 2.2, 4.5};  // writing the 32-bit partial results of a piece
+constexpr double kCombineCost = 3.0;              // the combine launch,
+constexpr double kCombineSlot = 0.025;            // and reading a piece's results there
 constexpr int kMaxSplit = 32;
 constexpr size_t kSplitItems = 2048;   // launches of more items are not cut (eight rounds of 256)
 
@@ -40,13 +41,13 @@ int pieces_of(const Unit& u, double cap) {
 // When the last of the launch's pieces ends, launched longest first on 256 compute units.
 double replay(const std::vector<Unit>& units, double cap) {
   std::vector<double> c;
-  bool split = false;
+  double combine = 0;
   for (const Unit& u : units) {
     const int n = pieces_of(u, cap);
-    split |= n > 1;
+    if (n > 1) combine += n * kCombineSlot * (u.it.kind == kDkv ? 2 : 1);
     for (int i = 0; i < n; ++i) {
       const int steps = u.steps * (i + 1) / n - u.steps * i / n;
-      c.push_back(kItemCost + steps * kStepCost[u.it.kind] + (n > 1 ? kSlotCost[u.it.kind] : 0.0));
+      c.push_back(kItemCost[u.it.kind] + steps * kStepCost[u.it.kind] + (n > 1 ? kSlotCost[u.it.kind] : 0.0));
     }
   }
   std::sort(c.begin(), c.end(), std::greater<double>());
@@ -59,7 +60,7 @@ double replay(const std::vector<Unit>& units, double cap) {
     cu.push(t);
     end = std::max(end, t);
   }
-  return end + (split ? kCombineCost : 0.0);
+  return end + (combine > 0 ? kCombineCost + combine : 0.0);
 }
 
 double choose_cap(const std::vector<Unit>& units) {
@@ -67,7 +68,7 @@ double choose_cap(const std::vector<Unit>& units) {
   double total = 0;
   for (const Unit& u : units) total += u.cost();
   double best_cap = 0, best = replay(units, 0);
-  for (double f : {2.0, 1.4, 1.0, 0.8, 0.65, 0.5, 0.4, 0.33, 0.25}) {
+  for (double f : {2.0, 1.7, 1.4, 1.2, 1.0, 0.9, 0.8, 0.7, 0.6, 0.5, 0.4, 0.3, 0.2}) {
     const double cap = std::max(f * total / kNumCus, 4.0);
     const double t = replay(units, cap);
     if (t < 0.97 * best) best = t, best_cap = cap;
@@ -109,23 +110,25 @@ void emit(const std::vector<Unit>& units, double cap, std::vector<CausalItem>* i
 
 void build_causal_tables(CausalTables* t) {
   const int32_t G = t->heads / t->kv_heads;
+  int64_t n = 0;
+  for (int32_t nq : t->nq) n += (int64_t(nq) * G + kCausalTile - 1) / kCausalTile * t->kv_heads;
+  // Launches that are not cut anyway take larger forward items.
+  t->fwd_tile = n > int64_t(kSplitItems) ? fwd_large_tile(t->head_dim) : kCausalTile;
   std::vector<Unit> fwd, dq, dkv;
   int32_t q0 = 0, k0 = 0;
   for (int32_t b = 0; b < t->batch; ++b) {
     const int32_t nq = t->nq[b], nk = t->nk[b];
     const int32_t rows = nq * G;
-    for (int32_t r = 0; r < rows; r += kCausalTile) {
-      const int32_t len = std::min(kCausalTile, rows - r);
-      const int32_t keys = std::max(0, (r + len - 1) / G + nk - nq + 1);  // seen by the last row
-      for (int32_t h = 0; h < t->kv_heads; ++h) {
-        const CausalItem it{kForward, h, r, len, q0, nq, k0, nk, 0, keys, 0, b};
-        fwd.push_back({it, (keys + 63) / 64});
-        if (t->backward) {
-          dq.push_back(fwd.back());
-          dq.back().it.kind = kDq;
-        }
+    auto row_items = [&](CausalKind kind, int32_t tile, std::vector<Unit>* out) {
+      for (int32_t r = 0; r < rows; r += tile) {
+        const int32_t len = std::min(tile, rows - r);
+        const int32_t keys = std::max(0, (r + len - 1) / G + nk - nq + 1);  // seen by the last row
+        for (int32_t h = 0; h < t->kv_heads; ++h)
+          out->push_back({CausalItem{kind, h, r, len, q0, nq, k0, nk, 0, keys, 0, b}, (keys + 63) / 64});
       }
-    }
+    };
+    row_items(kForward, t->fwd_tile, &fwd);
+    if (t->backward) row_items(kDq, kCausalTile, &dq);
     if (t->backward)
       for (int32_t k = 0; k < nk; k += kCausalTile) {
         CausalItem it{kDkv, 0, k, std::min(kCausalTile, nk - k), q0, nq, k0, nk, 0, 0, 0, b};

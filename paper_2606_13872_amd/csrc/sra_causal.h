@@ -22,7 +22,7 @@ struct CausalItem {
   int32_t kind;
   int32_t kvh;     // K/V head
   int32_t start;
-  int32_t len;     // <= 256
+  int32_t len;     // <= 256 (forward: <= CausalTables::fwd_tile)
   int32_t q0, nq;  // packed row of the sequence's first token, tokens
   int32_t k0, nk;  // packed row of its first key, keys
   int32_t lo, hi;
@@ -72,6 +72,7 @@ struct CausalTables {
   std::vector<int32_t> nq, nk;
   int64_t q_rows = 0, k_rows = 0;  // packed tokens, packed keys
   std::vector<CausalItem> fwd, fwd_combine, grad, grad_combine;
+  int32_t fwd_tile = kCausalTile;  // rows per forward item
   int32_t fwd_slots = 0, q_slots = 0, kv_slots = 0;
 };
 

@@ -460,6 +460,7 @@ __global__ void __launch_bounds__(kThreads) sra_causal_grad_combine_kernel(Causa
   if (r >= it.len) return;
   auto sum = [&](const float* p, int64_t slot, float scale, __bf16* dst) {
     floatx4 x = *reinterpret_cast<const floatx4*>(p);
+#pragma unroll 4
     for (int i = 1; i < it.hi; ++i) x += *reinterpret_cast<const floatx4*>(p + i * slot);
     bf16x4 y;
 #pragma unroll

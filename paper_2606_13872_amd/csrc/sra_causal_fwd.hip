@@ -3,7 +3,8 @@
 //   S = scale Q K^T on the keys j <= i + nk - nq of token i, LSE = ln sum exp S, O = exp(S - LSE) V,
 //
 // one pass over the keys with a running maximum and sum. One workgroup (8 wave64s, two per SIMD) takes one work
-// item (sra_causal.h): up to 256 (token, head of the group) rows, 32 per wave, against the keys up to the last
+// item (sra_causal.h): up to 256 (token, head of the group) rows, 32 per wave (long launches: 384, or 512 of 64 head
+// dims, which read and load the keys less often), against the keys up to the last
 // that its rows see. The key tiles that every row sees run through the software pipeline of sra_fwd_pipe.h; those
 // on the diagonal (256 / G tokens wide) run behind it, three at a time, masked by each row's last key. Rows that
 // see nothing (nq > nk) end with l = 0: O = 0, LSE = -inf.
@@ -13,11 +14,6 @@
 #include "sra_fwd_pipe.h"
 
 namespace sra {
-
-namespace {
-constexpr int kRowsPerWave = kCausalTile / kWaves;
-constexpr int kNQ = kRowsPerWave / 16;
-}  // namespace
 
 // A 32-key half whose first key is key0: row block qb sees the keys up to lim[qb]. P of hidden keys is 0.
 template <int D, int NQ>
@@ -36,10 +32,11 @@ __device__ __forceinline__ void causal_half(FwdState<D, NQ>& st, const __bf16* k
   pv_half<D, NQ>(st, vt, pack_half<NQ>(s));
 }
 
-template <int D>
+// kOneStride: k and v share one token stride, so one set of load offsets serves both.
+template <int D, int NQ, bool kOneStride>
 __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 sra_causal_fwd_kernel(CausalArgs a) {
-  constexpr int NQ = kNQ, NC = D / 32, ND = D / 16, BK = kFwdKeyStep, RK = kPadRS<D>;
+  constexpr int kRowsPerWave = 16 * NQ, NC = D / 32, ND = D / 16, BK = kFwdKeyStep, RK = kPadRS<D>;
   constexpr int KE = KTile<D>::kElems;
   __shared__ __attribute__((aligned(1024))) __bf16 kbuf0[KE];
   __shared__ __attribute__((aligned(1024))) __bf16 kbuf1[KE];
@@ -59,12 +56,10 @@ sra_causal_fwd_kernel(CausalArgs a) {
   const float sl2 = a.scale_log2;
 
   FwdState<D, NQ> st;
-  int lim[NQ];  // the last key that this lane's row sees (-1 and below: none)
 #pragma unroll
   for (int qb = 0; qb < NQ; ++qb) {
     const int r = wrow0 + 16 * qb + l16, row = it.start + min(r, it.len - 1);
     const int token = row / G, hg = row - token * G;
-    lim[qb] = token + off;
     const __bf16* src = a.q + int64_t(it.q0 + token) * a.qs + int64_t(it.kvh * G + hg) * D + g * 8;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
@@ -84,16 +79,13 @@ sra_causal_fwd_kernel(CausalArgs a) {
   // direct loads of a whole tile: K and V bases as uniform scalars, this lane's byte offsets from the first row
   using TL = PaddedTile<D, BK, RK>;
   constexpr int kSlots = (TL::kInstr + kWaves - 1) / kWaves, kFull = TL::kInstr / kWaves;
-  uint32_t koff[kSlots], voff[kSlots];
-  {
-    TileLoader<D, BK, RK, kWaves> tk, tv;
-    tk.init(a.ks, 0, wave);
-    tv.init(a.vs, 0, wave);
+  uint32_t offs[kOneStride ? 1 : 2][kSlots];
 #pragma unroll
-    for (int j = 0; j < kSlots; ++j) {
-      koff[j] = uint32_t(tk.voff[j]) * 2;
-      voff[j] = uint32_t(tv.voff[j]) * 2;
-    }
+  for (int s = 0; s < (kOneStride ? 1 : 2); ++s) {
+    TileLoader<D, BK, RK, kWaves> tl;
+    tl.init(s ? a.vs : a.ks, 0, wave);
+#pragma unroll
+    for (int j = 0; j < kSlots; ++j) offs[s][j] = uint32_t(tl.voff[j]) * 2;
   }
   const __bf16* const k0 = a.k + int64_t(it.k0) * a.ks + int64_t(it.kvh) * D;
   const __bf16* const v0 = a.v + int64_t(it.k0) * a.vs + int64_t(it.kvh) * D;
@@ -101,18 +93,18 @@ sra_causal_fwd_kernel(CausalArgs a) {
   uint64_t vp = uniform_u64(reinterpret_cast<uint64_t>(v0 + int64_t(it.lo) * a.vs));
   const uint64_t kstep = uint64_t(a.ks) * (2 * BK), vstep = uint64_t(a.vs) * (2 * BK);
   const bool extra = wave + kFull * kWaves < TL::kInstr;
-  auto issue = [&](uint64_t base, const uint32_t* offs, const __bf16* dst) __attribute__((always_inline)) {
+  auto issue = [&](uint64_t base, const uint32_t* off16, const __bf16* dst) __attribute__((always_inline)) {
     const uint32_t la = lds_addr(dst) + wave * 1024;
 #pragma unroll
     for (int j = 0; j < kSlots; ++j)
-      if (j < kFull || extra) lds_dma_x4_off(base, offs[j], la + j * kWaves * 1024);
+      if (j < kFull || extra) lds_dma_x4_off(base, off16[j], la + j * kWaves * 1024);
   };
   auto issue_k = [&](const __bf16* dst) __attribute__((always_inline)) {
-    issue(kp, koff, dst);
+    issue(kp, offs[0], dst);
     kp += kstep;
   };
   auto issue_v = [&](const __bf16* dst) __attribute__((always_inline)) {
-    issue(vp, voff, dst);
+    issue(vp, offs[kOneStride ? 0 : 1], dst);
     vp += vstep;
   };
 
@@ -175,6 +167,9 @@ sra_causal_fwd_kernel(CausalArgs a) {
   // The other tiles: on the diagonal, or ragged. Rows past hi are clamped to the last key before it; no row sees
   // them (hi is behind the last key of the item's last row, or a multiple of 64 away from lo).
   const int wlast = __builtin_amdgcn_readfirstlane((it.start + min(wrow0 + kRowsPerWave, it.len) - 1) / G + off);
+  int lim[NQ];  // the last key that this lane's row sees (-1 and below: none)
+#pragma unroll
+  for (int qb = 0; qb < NQ; ++qb) lim[qb] = (it.start + min(wrow0 + 16 * qb + l16, it.len - 1)) / G + off;
   for (int key0 = it.lo + BK * T; key0 < it.hi; key0 += 3 * BK) {
     __syncthreads();  // every wave is done with the buffers
 #pragma unroll
@@ -186,14 +181,14 @@ sra_causal_fwd_kernel(CausalArgs a) {
     wait_vmem();
     __syncthreads();
     if (active)
-#pragma unroll
-      for (int j = 0; j < 3; ++j)
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const int key = key0 + j * BK + half * 32;
-          if (key < it.hi && key <= wlast)
-            causal_half<D, NQ>(st, kb[j] + half * 32 * RK, vb[j] + half * 32 * RK, key, lim, sl2);
-        }
+#pragma unroll 1
+      for (int o = 0; o < 6; ++o) {  // one body for the halves: short calls wait for instructions
+        const int key = key0 + 32 * o, j = o >> 1;
+        if (key >= it.hi || key > wlast) break;
+        const __bf16* const kt = j == 0 ? kbuf0 : j == 1 ? kbuf1 : kbuf2;
+        const __bf16* const vt = j == 0 ? vbuf0 : j == 1 ? vbuf1 : vbuf2;
+        causal_half<D, NQ>(st, kt + (o & 1) * 32 * RK, vt + (o & 1) * 32 * RK, key, lim, sl2);
+      }
   }
 
   if (!active) return;
@@ -223,9 +218,8 @@ sra_causal_fwd_kernel(CausalArgs a) {
   }
 }
 
-// Rows of the split items from their pieces: with M the largest of the pieces' running maxima,
-// O = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i, in piece order. D / 4 threads per row. Bound by reading the
-// partial results.
+// Rows of the split items from their pieces, in piece order: with M the largest of the pieces' running maxima,
+// O = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i. D / 4 threads per row. Bound by reading the partial results.
 template <int D>
 __global__ void __launch_bounds__(kThreads) sra_causal_fwd_combine_kernel(CausalArgs a, const CausalItem* items) {
   constexpr int TPR = D / 4, RPB = kThreads / TPR;
@@ -234,15 +228,18 @@ __global__ void __launch_bounds__(kThreads) sra_causal_fwd_combine_kernel(Causal
   if (r >= it.len) return;
   constexpr int64_t slot = int64_t(kCausalTile) * (D + 2);
   const float* p = a.part + it.lo * slot;
-  float m = -INFINITY;
-  for (int i = 0; i < it.hi; ++i) m = fmaxf(m, p[i * slot + int64_t(kCausalTile) * D + 2 * r]);
+  float m = -INFINITY, l = 0.f;
   floatx4 o = floatx4{};
-  float l = 0.f;
-  for (int i = 0; i < it.hi; ++i) {
+#pragma unroll 4
+  for (int i = 0; i < it.hi; ++i) {  // one pass with a running maximum: the loads of four pieces are under way at once
     const float2 ml = *reinterpret_cast<const float2*>(p + i * slot + int64_t(kCausalTile) * D + 2 * r);
-    const float w = ml.y == 0.f ? 0.f : fast_exp2(ml.x - m);  // a piece that the row sees nothing of has m = -inf
-    l += w * ml.y;
-    o += w * *reinterpret_cast<const floatx4*>(p + i * slot + r * D + 4 * sub);
+    const floatx4 x = *reinterpret_cast<const floatx4*>(p + i * slot + r * D + 4 * sub);
+    const float mx = fmaxf(m, ml.x);
+    const float f = l == 0.f ? 0.f : fast_exp2(m - mx);  // nothing so far
+    const float w = ml.y == 0.f ? 0.f : fast_exp2(ml.x - mx);  // a piece that the row sees nothing of has m = -inf
+    l = f * l + w * ml.y;
+    o = f * o + w * x;
+    m = mx;
   }
   const int G = a.heads / a.kv_heads, row = it.start + r, token = row / G, h = it.kvh * G + row - token * G;
   const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -253,11 +250,23 @@ __global__ void __launch_bounds__(kThreads) sra_causal_fwd_combine_kernel(Causal
   if (sub == 0) a.lse[int64_t(h) * a.q_rows + it.q0 + token] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-hipError_t launch_causal_forward(const CausalArgs& a, int n_items, int head_dim, hipStream_t stream) {
-  if (n_items <= 0) return hipSuccess;
+template <int D, int NQ>
+static void launch_tile(const CausalArgs& a, int n_items, hipStream_t stream) {
   const dim3 grid(n_items), block(kWaves * 64);
-  if (head_dim == 128) hipLaunchKernelGGL(sra_causal_fwd_kernel<128>, grid, block, 0, stream, a);
-  else hipLaunchKernelGGL(sra_causal_fwd_kernel<64>, grid, block, 0, stream, a);
+  if (a.ks == a.vs) hipLaunchKernelGGL((sra_causal_fwd_kernel<D, NQ, true>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((sra_causal_fwd_kernel<D, NQ, false>), grid, block, 0, stream, a);
+}
+
+hipError_t launch_causal_forward(const CausalArgs& a, int n_items, int head_dim, int tile, hipStream_t stream) {
+  if (n_items <= 0) return hipSuccess;
+  constexpr int kRows = 16 * kWaves;
+  if (head_dim == 128) {
+    if (tile == kCausalTile) launch_tile<128, kCausalTile / kRows>(a, n_items, stream);
+    else launch_tile<128, fwd_large_tile(128) / kRows>(a, n_items, stream);
+  } else {
+    if (tile == kCausalTile) launch_tile<64, kCausalTile / kRows>(a, n_items, stream);
+    else launch_tile<64, fwd_large_tile(64) / kRows>(a, n_items, stream);
+  }
   return hipGetLastError();
 }
 

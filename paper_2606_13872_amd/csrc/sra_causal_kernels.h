@@ -34,7 +34,8 @@ struct CausalDeltaArgs {
   int32_t q_rows, heads;
 };
 
-hipError_t launch_causal_forward(const CausalArgs& a, int n_items, int head_dim, hipStream_t stream);
+// tile: rows per item
+hipError_t launch_causal_forward(const CausalArgs& a, int n_items, int head_dim, int tile, hipStream_t stream);
 hipError_t launch_causal_forward_combine(const CausalArgs& a, const CausalItem* items, int n, int head_dim,
                                          hipStream_t stream);
 hipError_t launch_causal_delta(const CausalDeltaArgs& a, int head_dim, hipStream_t stream);

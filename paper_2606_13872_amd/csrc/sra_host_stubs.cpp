@@ -20,7 +20,7 @@ hipError_t launch_grad_combine(const BwdArgs&, const CombineItem*, int, int, int
 hipError_t launch_fill(const FillArgs&, hipStream_t) { return hipErrorNotSupported; }
 hipError_t launch_gather(const GatherArgs&, hipStream_t) { return hipErrorNotSupported; }
 hipError_t launch_scatter(const ScatterArgs&, hipStream_t) { return hipErrorNotSupported; }
-hipError_t launch_causal_forward(const CausalArgs&, int, int, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_causal_forward(const CausalArgs&, int, int, int, hipStream_t) { return hipErrorNotSupported; }
 hipError_t launch_causal_forward_combine(const CausalArgs&, const CausalItem*, int, int, hipStream_t) {
   return hipErrorNotSupported;
 }

@@ -314,7 +314,7 @@ sra_status sra_causal_forward(const sra_causal_plan* plan, const void* tables, c
   a.lse = lse;
   a.part = static_cast<float*>(workspace);
   const hipError_t e = timed_launch(SRA_KERNEL_CAUSAL_FORWARD, s, [&] {
-    const hipError_t x = launch_causal_forward(a, int(t.fwd.size()), t.head_dim, s);
+    const hipError_t x = launch_causal_forward(a, int(t.fwd.size()), t.head_dim, t.fwd_tile, s);
     if (x != hipSuccess) return x;
     return launch_causal_forward_combine(a, table(plan, tables, 1), int(t.fwd_combine.size()), t.head_dim, s);
   });

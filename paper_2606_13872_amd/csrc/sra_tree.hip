@@ -770,16 +770,19 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_combine_kernel(TreeArgs
   const int r = blockIdx.y * RPB + threadIdx.x / TPR, sub = threadIdx.x % TPR;
   if (sp.pieces == 0 || r >= sp.rows) return;
   auto piece = [&](int i) { return a.part + kSlot * (2 * (w + i) + (i == 0)); };
-  float m = -INFINITY;
-  for (int i = 0; i < sp.pieces; ++i) m = fmaxf(m, piece(i)[R * D + 2 * r]);
+  float m = -INFINITY, l = 0.f;
   floatx4 o = floatx4{};
-  float l = 0.f;
-  for (int i = 0; i < sp.pieces; ++i) {
+#pragma unroll 4
+  for (int i = 0; i < sp.pieces; ++i) {  // one pass with a running maximum: the loads of four pieces are under way at once
     const float* p = piece(i);
-    const float2 x = *reinterpret_cast<const float2*>(p + R * D + 2 * r);
-    const float f = x.y == 0.f ? 0.f : fast_exp2(x.x - m);
-    l += f * x.y;
-    o += f * *reinterpret_cast<const floatx4*>(p + r * D + 4 * sub);
+    const float2 ml = *reinterpret_cast<const float2*>(p + R * D + 2 * r);
+    const floatx4 x = *reinterpret_cast<const floatx4*>(p + r * D + 4 * sub);
+    const float mx = fmaxf(m, ml.x);
+    const float f = l == 0.f ? 0.f : fast_exp2(m - mx);        // nothing so far
+    const float e = ml.y == 0.f ? 0.f : fast_exp2(ml.x - mx);  // a piece that the row sees nothing of has m = -inf
+    l = f * l + e * ml.y;
+    o = f * o + e * x;
+    m = mx;
   }
   const int G = a.heads / a.c.kv_heads, rr = sp.row0 + r, token = rr / G, h = sp.kvh * G + rr - token * G;
   const float inv = l == 0.f ? 0.f : 1.f / l;
