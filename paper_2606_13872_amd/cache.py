@@ -12,7 +12,7 @@ from typing import Dict, Optional
 import numpy as np
 
 from . import sra as _s
-from .causal import _call, _no_alias, _stride
+from .causal import _call, _no_alias
 
 _declared = False
 
@@ -45,58 +45,69 @@ def _lib():
     return L
 
 
-def _ints(t, name, dims):
-    """An int32 tensor of so many dims (or, 8 bytes wide, the tree masks) with contiguous entries."""
-    torch = _s._tm()
-    want = torch.int64 if name == "tree" else torch.int32
-    if not isinstance(t, torch.Tensor) or t.dtype != want or t.dim() != dims:
-        raise _s._bad(f"{name} must be a {dims}-dimensional {want} tensor")
+def _ints(t, name, dims, dtype):
+    """An integer tensor of so many dims with contiguous entries."""
+    if not isinstance(t, _s._tm().Tensor) or t.dtype != dtype or t.dim() != dims:
+        raise _s._bad(f"{name} must be a {dims}-dimensional {dtype} tensor")
     if t.shape[-1] > 1 and t.stride(-1) != 1:
         raise _s._bad(f"{name}: entries must be contiguous")
+
+
+def _pages(t, name, shape, kv_heads, head_dim):
+    """Page and token strides of a cache tensor (0: it has one page)."""
+    torch = _s._tm()
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16 or t.dim() != 4:
+        raise _s._bad(f"{name} must be a bfloat16 [pages, page_size, kv_heads, head_dim] tensor")
+    if t.shape != shape or shape[2] != kv_heads or shape[3] != head_dim:
+        raise _s._bad(f"{name}: shape {tuple(t.shape)}, expected [pages, page_size, {kv_heads}, {head_dim}]")
+    st, row = t.stride(), kv_heads * head_dim
+    if shape[0] and shape[1]:
+        if st[3] != 1 or (kv_heads > 1 and st[2] != head_dim):
+            raise _s._bad(f"{name} must have contiguous heads")
+        if st[1] < row or (shape[0] > 1 and st[0] < (shape[1] - 1) * st[1] + row):
+            raise _s._bad(f"{name}: tokens or pages overlap")
+    return st[0] if shape[0] > 1 else 0, st[1]
 
 
 def _cache(k_cache, v_cache, page_table, context_lens, cu_tokens, tokens, kv_heads, head_dim):
     """The checked sra_paged_cache of the tensors."""
     torch = _s._tm()
-    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
-        if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16 or t.dim() != 4:
-            raise _s._bad(f"{name} must be a bfloat16 [pages, page_size, kv_heads, head_dim] tensor")
-        if t.shape != k_cache.shape or t.shape[2:] != (kv_heads, head_dim):
-            raise _s._bad(f"{name}: shape {tuple(t.shape)}, expected [pages, page_size, {kv_heads}, {head_dim}]")
-        if t.numel() and (t.stride(3) != 1 or (kv_heads > 1 and t.stride(2) != head_dim)):
-            raise _s._bad(f"{name} must have contiguous heads")
-        if t.numel() and (t.stride(1) < kv_heads * head_dim or
-                          (t.shape[0] > 1 and t.stride(0) < (t.shape[1] - 1) * t.stride(1) + kv_heads * head_dim)):
-            raise _s._bad(f"{name}: tokens or pages overlap")
-    _ints(page_table, "page_table", 2)
-    _ints(context_lens, "context_lens", 1)
-    _ints(cu_tokens, "cu_tokens", 1)
+    if not isinstance(k_cache, torch.Tensor):
+        raise _s._bad("k_cache must be a torch tensor")
+    shape = k_cache.shape
+    kp, kt = _pages(k_cache, "k_cache", shape, kv_heads, head_dim)
+    vp, vt = _pages(v_cache, "v_cache", shape, kv_heads, head_dim)
+    _ints(page_table, "page_table", 2, torch.int32)
+    _ints(context_lens, "context_lens", 1, torch.int32)
+    _ints(cu_tokens, "cu_tokens", 1, torch.int32)
     n = context_lens.shape[0]
-    if page_table.shape[0] != n or cu_tokens.shape[0] != n + 1:
+    rows, width = page_table.shape
+    if rows != n or cu_tokens.shape[0] != n + 1:
         raise _s._bad("page_table needs one row and cu_tokens one entry more than context_lens has")
-    if n > 1 and page_table.stride(0) < page_table.shape[1]:
+    ts = page_table.stride(0) if n > 1 else 0
+    if n > 1 and ts < width:
         raise _s._bad("page_table: rows overlap")
-    pages, page = k_cache.shape[:2]
-    # a single page (or token of a page) has no stride of its own
-    kp, vp = (t.stride(0) if pages > 1 else 0 for t in (k_cache, v_cache))
-    c = _PagedCache(n, tokens, kv_heads, head_dim, pages, page, page_table.shape[1], _addr(k_cache), _addr(v_cache),
-                    kp, vp, k_cache.stride(1), v_cache.stride(1), _addr(page_table),
-                    page_table.stride(0) if n > 1 else 0, _addr(context_lens), _addr(cu_tokens))
-    return c, (("k_cache", k_cache), ("v_cache", v_cache), ("page_table", page_table), ("context_lens", context_lens),
-               ("cu_tokens", cu_tokens))
+    return _PagedCache(n, tokens, kv_heads, head_dim, shape[0], shape[1], width, _addr(k_cache), _addr(v_cache),
+                       kp, vp, kt, vt, _addr(page_table), ts, _addr(context_lens), _addr(cu_tokens))
 
 
 def _addr(t):
     return t.data_ptr() if t is not None and t.numel() else None
 
 
-def _end(t):
-    return t.data_ptr() + t.element_size() * (sum((n - 1) * s for n, s in zip(t.shape, t.stride())) + 1)
-
-
 def _rows(t, name, shape):
-    _s._expect(t, name, shape, _s._tm().bfloat16, False)
-    return _stride(t, name)
+    """Token stride of bf16 [tokens, heads, head_dim] with contiguous heads (0: at most one token)."""
+    torch = _s._tm()
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16 or t.shape != shape:
+        _s._expect(t, name, shape, torch.bfloat16, False)  # says what is wrong
+    st = t.stride()
+    if shape[0] and (st[2] != 1 or (shape[1] > 1 and st[1] != shape[2])):
+        raise _s._bad(f"{name} must be [tokens, heads, head_dim] with contiguous heads")
+    if shape[0] <= 1:
+        return 0
+    if st[0] < shape[1] * shape[2]:
+        raise _s._bad(f"{name}: tokens overlap (stride {st[0]})")
+    return st[0]
 
 
 def _dims(t, name):
@@ -123,28 +134,50 @@ def tree_attention(q, k, v, k_cache, v_cache, page_table, context_lens, cu_token
     torch = _s._tm()
     tokens, heads, d = _dims(q, "q")
     kv = _dims(k, "k")[1]
-    qs, ks, vs = _rows(q, "q", (tokens, heads, d)), _rows(k, "k", (tokens, kv, d)), _rows(v, "v", (tokens, kv, d))
-    c, tensors = _cache(k_cache, v_cache, page_table, context_lens, cu_tokens, tokens, kv, d)
+    shape, kv_shape = (tokens, heads, d), (tokens, kv, d)
+    qs, ks, vs = _rows(q, "q", shape), _rows(k, "k", kv_shape), _rows(v, "v", kv_shape)
+    c = _cache(k_cache, v_cache, page_table, context_lens, cu_tokens, tokens, kv, d)
     if tree is not None:
-        _ints(tree, "tree", 1)
+        _ints(tree, "tree", 1, torch.int64)
         if tree.shape[0] != tokens:
             raise _s._bad("tree needs one mask per token")
-    _s._precheck_outs(out, [("o", (tokens, heads, d), torch.bfloat16), ("lse", (heads, tokens), torch.float32)])
-    n = ctypes.c_size_t()
-    _s._check(_lib().sra_tree_workspace_size(ctypes.byref(c), heads, ctypes.byref(n)))
-    dev = q.device
-    ins = (("q", q), ("k", k), ("v", v), ("tree", tree)) + tensors
-    _s._same_device(ins, dev)
-    out = out or {}
-    o = _s._out(out, "o", (tokens, heads, d), torch.bfloat16, dev)
-    lse = _s._out(out, "lse", (heads, tokens), torch.float32, dev)
-    ws = _s._workspace(out, n.value, dev)
     if out:
+        _s._precheck_outs(out, [("o", shape, torch.bfloat16), ("lse", (heads, tokens), torch.float32)])
+    nbytes = _workspace_size(c, heads)
+    dev = q.device
+    ins = (("q", q), ("k", k), ("v", v), ("tree", tree), ("k_cache", k_cache), ("v_cache", v_cache),
+           ("page_table", page_table), ("context_lens", context_lens), ("cu_tokens", cu_tokens))
+    _s._same_device(ins, dev)
+    if out:
+        o = _s._out(out, "o", shape, torch.bfloat16, dev)
+        lse = _s._out(out, "lse", (heads, tokens), torch.float32, dev)
+        ws = _s._workspace(out, nbytes, dev)
         _no_alias(out, ins + (("o", o), ("lse", lse), ("workspace", ws)))
+    else:
+        o = torch.empty(shape, dtype=torch.bfloat16, device=dev)
+        lse = torch.empty((heads, tokens), dtype=torch.float32, device=dev)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
     _s._check(_call(dev, lambda s: _lib().sra_tree_attention(
-        ctypes.byref(c), heads, _addr(q), _addr(k), _addr(v), qs, ks, vs, _addr(tree), _addr(o), _addr(lse),
-        0.0 if scale is None else float(scale), _addr(ws), ws.numel(), s)))
+        c, heads, _addr(q), _addr(k), _addr(v), qs, ks, vs, _addr(tree), _addr(o), _addr(lse),
+        0.0 if scale is None else float(scale), ws.data_ptr(), ws.numel(), s)))
     return o, lse
+
+
+_SIZES: Dict[tuple, int] = {}
+
+
+def _workspace_size(c, heads):
+    """sra_tree_workspace_size, asked once per set of sizes."""
+    key = (c.batch, c.tokens, c.num_kv_heads, c.head_dim, c.num_pages, c.page_size, c.max_pages, c.table_stride,
+           c.k_page_stride, c.v_page_stride, c.k_token_stride, c.v_token_stride, heads)
+    n = _SIZES.get(key)
+    if n is None:
+        size = ctypes.c_size_t()
+        _s._check(_lib().sra_tree_workspace_size(c, heads, ctypes.byref(size)))
+        if len(_SIZES) >= 4096:
+            _SIZES.clear()
+        n = _SIZES[key] = size.value
+    return n
 
 
 def cache_append(k, v, k_cache, v_cache, page_table, context_lens, cu_tokens, rows=None):
@@ -160,30 +193,33 @@ def cache_append(k, v, k_cache, v_cache, page_table, context_lens, cu_tokens, ro
     ks, vs = _rows(k, "k", (n, kv, d)), _rows(v, "v", (n, kv, d))
     tokens = n
     if rows is not None:
-        _ints(rows, "rows", 1)
+        _ints(rows, "rows", 1, _s._tm().int32)
         tokens = rows.shape[0]
-    c, tensors = _cache(k_cache, v_cache, page_table, context_lens, cu_tokens, tokens, kv, d)
+    c = _cache(k_cache, v_cache, page_table, context_lens, cu_tokens, tokens, kv, d)
     dev = k.device
-    ins = (("k", k), ("v", v), ("rows", rows)) + tensors
-    for name, t in (("k", k), ("v", v)):  # rows are read while others are written
-        for other, cache in tensors[:2]:
-            if t.numel() and cache.numel() and _end(t) > cache.data_ptr() and _end(cache) > t.data_ptr():
-                raise _s._bad(f"{name} overlaps {other}")
-    _s._same_device(ins, dev)
-    _s._check(_call(dev, lambda s: _lib().sra_cache_append(ctypes.byref(c), _addr(k), _addr(v), ks, vs, _addr(rows), n, s)))
+    if n and c.num_pages:  # rows are read while others are written
+        spans = [(t.data_ptr(), t.data_ptr() + 2 * ((t.shape[0] - 1) * s + kv * d)) for t, s in ((k, ks), (v, vs))]
+        for cache, ps, ts in ((k_cache, c.k_page_stride, c.k_token_stride), (v_cache, c.v_page_stride, c.v_token_stride)):
+            a = cache.data_ptr()
+            b = a + 2 * ((c.num_pages - 1) * ps + (c.page_size - 1) * ts + kv * d)
+            if any(lo < b and a < hi for lo, hi in spans):
+                raise _s._bad("k or v overlaps the cache")
+    _s._same_device((("k", k), ("v", v), ("rows", rows), ("k_cache", k_cache), ("v_cache", v_cache),
+                     ("page_table", page_table), ("context_lens", context_lens), ("cu_tokens", cu_tokens)), dev)
+    _s._check(_call(dev, lambda s: _lib().sra_cache_append(c, _addr(k), _addr(v), ks, vs, _addr(rows), n, s)))
 
 
 def cache_rows(k_cache, v_cache, page_table, context_lens, cu_tokens, tokens: int, sequence: int = 0):
     """sra_cache_rows on CPU tensors: (the cache row that each of `tokens` packed tokens is appended to, the cache rows
     of the positions of `sequence` up to its page_table row's end), -1 where there is none."""
     kv, d = _cache_dims(k_cache)
-    c, tensors = _cache(k_cache, v_cache, page_table, context_lens, cu_tokens, tokens, kv, d)
-    for name, t in tensors[2:]:
+    c = _cache(k_cache, v_cache, page_table, context_lens, cu_tokens, tokens, kv, d)
+    for name, t in (("page_table", page_table), ("context_lens", context_lens), ("cu_tokens", cu_tokens)):
         if t.device.type != "cpu":
             raise _s._bad(f"{name}: the hook reads host memory")
     a = np.full(max(tokens, 1), -1, dtype=np.int64)
     p = np.full(max(page_table.shape[1] * k_cache.shape[1], 1), -1, dtype=np.int64)
-    _s._check(_lib().sra_cache_rows(ctypes.byref(c), a.ctypes.data, sequence, p.ctypes.data))
+    _s._check(_lib().sra_cache_rows(c, a.ctypes.data, sequence, p.ctypes.data))
     return a[:tokens], p
 
 
