@@ -23,13 +23,18 @@ constexpr double kItemCost[3] = {2.9, 4.5, 6.0};  // an item's loads before the 
 constexpr double kSlotCost[3] = {2.2, 2.2, 4.5};  // writing the 32-bit partial results of a piece
 constexpr double kCombineCost = 3.0;              // the combine launch,
 constexpr double kCombineSlot = 0.025;            // and reading a piece's results there
+// A step of a large forward item (384 or 512 rows) to one of 256 rows: 0.93 times the work's share.
+constexpr double large_step(int head_dim) { return 0.93 * fwd_large_tile(head_dim) / kCausalTile; }
+// Steps of 64 head dims take 0.6 times as long, what does not depend on them is worth more of them.
+constexpr double fixed_cost(int head_dim) { return head_dim == 128 ? 1.0 : 1.7; }
 constexpr int kMaxSplit = 32;
 constexpr size_t kSplitItems = 2048;   // launches of more items are not cut (eight rounds of 256)
 
 struct Unit {
   CausalItem it;
   int32_t steps;
-  double cost() const { return steps * kStepCost[it.kind]; }
+  double step;  // cost of one
+  double cost() const { return steps * step; }
 };
 
 int pieces_of(const Unit& u, double cap) {
@@ -39,7 +44,7 @@ int pieces_of(const Unit& u, double cap) {
 }
 
 // When the last of the launch's pieces ends, launched longest first on 256 compute units.
-double replay(const std::vector<Unit>& units, double cap) {
+double replay(const std::vector<Unit>& units, double cap, double fixed) {
   std::vector<double> c;
   double combine = 0;
   for (const Unit& u : units) {
@@ -47,7 +52,7 @@ double replay(const std::vector<Unit>& units, double cap) {
     if (n > 1) combine += n * kCombineSlot * (u.it.kind == kDkv ? 2 : 1);
     for (int i = 0; i < n; ++i) {
       const int steps = u.steps * (i + 1) / n - u.steps * i / n;
-      c.push_back(kItemCost[u.it.kind] + steps * kStepCost[u.it.kind] + (n > 1 ? kSlotCost[u.it.kind] : 0.0));
+      c.push_back(fixed * kItemCost[u.it.kind] + steps * u.step + (n > 1 ? kSlotCost[u.it.kind] : 0.0));
     }
   }
   std::sort(c.begin(), c.end(), std::greater<double>());
@@ -60,19 +65,20 @@ double replay(const std::vector<Unit>& units, double cap) {
     cu.push(t);
     end = std::max(end, t);
   }
-  return end + (combine > 0 ? kCombineCost + combine : 0.0);
+  return end + (combine > 0 ? fixed * kCombineCost + combine : 0.0);
 }
 
-double choose_cap(const std::vector<Unit>& units) {
-  if (units.empty() || units.size() > kSplitItems) return 0;
+// The cost from which on items are cut (0: none is), and when the launch then ends.
+double choose_cap(const std::vector<Unit>& units, double fixed, double* end) {
   double total = 0;
   for (const Unit& u : units) total += u.cost();
-  double best_cap = 0, best = replay(units, 0);
+  double best_cap = 0, best = replay(units, 0, fixed);
   for (double f : {2.0, 1.7, 1.4, 1.2, 1.0, 0.9, 0.8, 0.7, 0.6, 0.5, 0.4, 0.3, 0.2}) {
     const double cap = std::max(f * total / kNumCus, 4.0);
-    const double t = replay(units, cap);
+    const double t = replay(units, cap, fixed);
     if (t < 0.97 * best) best = t, best_cap = cap;
   }
+  if (end) *end = best;
   return best_cap;
 }
 
@@ -99,7 +105,7 @@ void emit(const std::vector<Unit>& units, double cap, std::vector<CausalItem>* i
         x.hi = std::min(64 * b, u.it.hi);
       }
       if (n > 1) x.slot = ++slots[u.it.kind];
-      out.emplace_back((b - a) * kStepCost[u.it.kind], x);
+      out.emplace_back((b - a) * u.step, x);
     }
   }
   std::stable_sort(out.begin(), out.end(), [](const auto& a, const auto& b) { return a.first > b.first; });
@@ -110,43 +116,51 @@ void emit(const std::vector<Unit>& units, double cap, std::vector<CausalItem>* i
 
 void build_causal_tables(CausalTables* t) {
   const int32_t G = t->heads / t->kv_heads;
-  int64_t n = 0;
-  for (int32_t nq : t->nq) n += (int64_t(nq) * G + kCausalTile - 1) / kCausalTile * t->kv_heads;
-  // Launches that are not cut anyway take larger forward items.
-  t->fwd_tile = n > int64_t(kSplitItems) ? fwd_large_tile(t->head_dim) : kCausalTile;
-  std::vector<Unit> fwd, dq, dkv;
-  int32_t q0 = 0, k0 = 0;
-  for (int32_t b = 0; b < t->batch; ++b) {
-    const int32_t nq = t->nq[b], nk = t->nk[b];
-    const int32_t rows = nq * G;
-    auto row_items = [&](CausalKind kind, int32_t tile, std::vector<Unit>* out) {
-      for (int32_t r = 0; r < rows; r += tile) {
-        const int32_t len = std::min(tile, rows - r);
-        const int32_t keys = std::max(0, (r + len - 1) / G + nk - nq + 1);  // seen by the last row
-        for (int32_t h = 0; h < t->kv_heads; ++h)
-          out->push_back({CausalItem{kind, h, r, len, q0, nq, k0, nk, 0, keys, 0, b}, (keys + 63) / 64});
+  const double fixed = fixed_cost(t->head_dim);
+  // Items of `tile` rows or keys each, K/V heads innermost.
+  auto units = [&](CausalKind kind, int32_t tile, double step) {
+    std::vector<Unit> out;
+    int32_t q0 = 0, k0 = 0;
+    for (int32_t b = 0; b < t->batch; ++b) {
+      const int32_t nq = t->nq[b], nk = t->nk[b], n = kind == kDkv ? nk : nq * G;
+      for (int32_t r = 0; r < n; r += tile) {
+        CausalItem it{kind, 0, r, std::min(tile, n - r), q0, nq, k0, nk, 0, 0, 0, b};
+        int32_t steps;
+        if (kind == kDkv) {
+          steps = it.hi = G * causal_tiles(it).n;
+        } else {
+          it.hi = std::max(0, (r + it.len - 1) / G + nk - nq + 1);  // keys seen by the last row
+          steps = (it.hi + 63) / 64;
+        }
+        for (it.kvh = 0; it.kvh < t->kv_heads; ++it.kvh) out.push_back({it, steps, step});
       }
-    };
-    row_items(kForward, t->fwd_tile, &fwd);
-    if (t->backward) row_items(kDq, kCausalTile, &dq);
-    if (t->backward)
-      for (int32_t k = 0; k < nk; k += kCausalTile) {
-        CausalItem it{kDkv, 0, k, std::min(kCausalTile, nk - k), q0, nq, k0, nk, 0, 0, 0, b};
-        it.hi = G * causal_tiles(it).n;
-        for (it.kvh = 0; it.kvh < t->kv_heads; ++it.kvh) dkv.push_back({it, it.hi});
-      }
-    q0 += nq;
-    k0 += nk;
-  }
+      q0 += nq;
+      k0 += nk;
+    }
+    return out;
+  };
   int32_t slots[3] = {0, 0, 0};
-  emit(fwd, choose_cap(fwd), &t->fwd, &t->fwd_combine, slots);
-  if (dq.size() + dkv.size() <= kSplitItems) {  // few items: both kinds together, each fills the other's gaps
-    std::vector<Unit> both(dkv);
-    both.insert(both.end(), dq.begin(), dq.end());
-    emit(both, choose_cap(both), &t->grad, &t->grad_combine, slots);
-  } else {  // many: one kind after the other, so that an XCD streams one kind of rows at a time
-    emit(dkv, 0, &t->grad, &t->grad_combine, slots);
-    emit(dq, 0, &t->grad, &t->grad_combine, slots);
+  std::vector<Unit> fwd = units(kForward, kCausalTile, kStepCost[kForward]);
+  double cap = 0, end = 0;
+  t->fwd_tile = fwd_large_tile(t->head_dim);
+  if (fwd.size() <= kSplitItems) {  // larger items, or these, cut or not: whichever end first
+    cap = choose_cap(fwd, fixed, &end);
+    if (end <= replay(units(kForward, t->fwd_tile, large_step(t->head_dim)), 0, fixed)) t->fwd_tile = kCausalTile;
+  }
+  if (t->fwd_tile != kCausalTile) {
+    fwd = units(kForward, t->fwd_tile, large_step(t->head_dim));
+    cap = 0;
+  }
+  emit(fwd, cap, &t->fwd, &t->fwd_combine, slots);
+  if (t->backward) {
+    std::vector<Unit> dkv = units(kDkv, kCausalTile, kStepCost[kDkv]), dq = units(kDq, kCausalTile, kStepCost[kDq]);
+    if (dq.size() + dkv.size() <= kSplitItems) {  // few items: both kinds together, each fills the other's gaps
+      dkv.insert(dkv.end(), dq.begin(), dq.end());
+      emit(dkv, choose_cap(dkv, fixed, nullptr), &t->grad, &t->grad_combine, slots);
+    } else {  // many: one kind after the other, so that an XCD streams one kind of rows at a time
+      emit(dkv, 0, &t->grad, &t->grad_combine, slots);
+      emit(dq, 0, &t->grad, &t->grad_combine, slots);
+    }
   }
   t->fwd_slots = slots[kForward];
   t->q_slots = slots[kDq];
