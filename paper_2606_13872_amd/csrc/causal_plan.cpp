@@ -10,7 +10,6 @@
 
 #include <algorithm>
 #include <functional>
-#include <queue>
 
 namespace sra {
 
@@ -46,6 +45,7 @@ int pieces_of(const Unit& u, double cap) {
 // When the last of the launch's pieces ends, launched longest first on 256 compute units.
 double replay(const std::vector<Unit>& units, double cap, double fixed) {
   std::vector<double> c;
+  c.reserve(units.size() * 2);
   double combine = 0;
   for (const Unit& u : units) {
     const int n = pieces_of(u, cap);
@@ -56,13 +56,17 @@ double replay(const std::vector<Unit>& units, double cap, double fixed) {
     }
   }
   std::sort(c.begin(), c.end(), std::greater<double>());
-  std::priority_queue<double, std::vector<double>, std::greater<double>> cu;
-  for (int i = 0; i < kNumCus; ++i) cu.push(0.0);
+  double heap[kNumCus] = {};  // when each compute unit is free; the first is the least
   double end = 0;
   for (double x : c) {
-    const double t = cu.top() + x;
-    cu.pop();
-    cu.push(t);
+    const double t = heap[0] + x;
+    int i = 0;
+    for (int k; (k = 2 * i + 1) < kNumCus; i = k) {
+      if (k + 1 < kNumCus && heap[k + 1] < heap[k]) ++k;
+      if (heap[k] >= t) break;
+      heap[i] = heap[k];
+    }
+    heap[i] = t;
     end = std::max(end, t);
   }
   return end + (combine > 0 ? fixed * kCombineCost + combine : 0.0);
@@ -73,7 +77,7 @@ double choose_cap(const std::vector<Unit>& units, double fixed, double* end) {
   double total = 0;
   for (const Unit& u : units) total += u.cost();
   double best_cap = 0, best = replay(units, 0, fixed);
-  for (double f : {2.0, 1.7, 1.4, 1.2, 1.0, 0.9, 0.8, 0.7, 0.6, 0.5, 0.4, 0.3, 0.2}) {
+  for (double f : {2.0, 1.5, 1.2, 1.1, 1.0, 0.8, 0.65, 0.5, 0.35}) {
     const double cap = std::max(f * total / kNumCus, 4.0);
     const double t = replay(units, cap, fixed);
     if (t < 0.97 * best) best = t, best_cap = cap;

@@ -23,6 +23,15 @@ def test_plan_covers_exactly_the_causal_mask(nq, nk, heads, kv):
         assert got.shape == want.shape and np.array_equal(got, want), (b, which, h)
 
 
+def test_long_launches_cover_exactly_the_causal_mask_in_larger_items():
+    nq = [900, 385, 1] + [5] * 300
+    for d in (64, 128):
+        plan = sra.CausalPlan(nq, 16, 8, d)
+        assert plan.forward_workspace == 0
+        for b, which, h in itertools.product((0, 1, 2, 200), range(3), (0, 15)):
+            assert np.array_equal(plan.mask(which, b, h), T.causal_mask(nq[b], nq[b]).numpy().astype(np.uint8))
+
+
 def test_long_items_of_short_launches_are_split_and_sizes_follow():
     whole = sra.CausalPlan([128] * 64, 8, 8, 128)
     assert whole.forward_workspace == 0

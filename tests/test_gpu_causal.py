@@ -68,6 +68,16 @@ def test_long_sequences(d):
     _check([2500, 311], [4000, 311], 2, 2, d, seed=4)
 
 
+@pytest.mark.parametrize("heads,kv,d", [(16, 8, 128), (8, 8, 64)])
+def test_many_sequences(heads, kv, d):
+    """Launches too long to be cut: the larger forward items, dK/dV and dQ one after the other."""
+    print("causal many", heads, kv, d, flush=True)
+    nq = [900, 385, 1, 513] + [3, 17] * 150
+    nk = [900, 500, 1, 600] + [3, 17] * 150
+    assert sum(-(-n * (heads // kv) // 256) for n in nq) * kv > 2048
+    _check(nq, nk, heads, kv, d, seed=15)
+
+
 @pytest.mark.parametrize("size,scale", [(3.0, None), (1.0, 1.0), (1.0, 0.02)])
 def test_peaked_and_flat_scores(size, scale):
     """Scores whose running maximum keeps rising, and custom scales."""
