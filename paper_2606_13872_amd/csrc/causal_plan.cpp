@@ -127,7 +127,8 @@ void build_causal_tables(CausalTables* t) {
     int32_t q0 = 0, k0 = 0;
     for (int32_t b = 0; b < t->batch; ++b) {
       const int32_t nq = t->nq[b], nk = t->nk[b], n = kind == kDkv ? nk : nq * G;
-      for (int32_t r = 0; r < n; r += tile) {
+      for (int64_t at = 0; at < n; at += tile) {
+        const int32_t r = int32_t(at);
         CausalItem it{kind, 0, r, std::min(tile, n - r), q0, nq, k0, nk, 0, 0, 0, b};
         int32_t steps;
         if (kind == kDkv) {

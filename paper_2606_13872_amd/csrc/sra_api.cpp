@@ -555,9 +555,8 @@ sra_status forward_call(const sra_problem* p, const void* q_gen, const void* k_g
 
 sra_status set_error(sra_status s, const char* msg) { return fail(s, msg); }
 
-hipError_t timed_launch(int kernel, hipStream_t stream, const std::function<hipError_t()>& launch) {
-  return timed(kernel, stream, launch);
-}
+hipEvent_t timing_begin(hipStream_t stream) { return timer().mark(stream); }
+void timing_end(int kernel, hipStream_t stream, hipEvent_t begin) { timer().add(kernel, begin, timer().mark(stream)); }
 
 }  // namespace sra
 

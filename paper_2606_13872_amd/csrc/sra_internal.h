@@ -3,8 +3,6 @@
 #include <hip/hip_runtime.h>
 #include <stddef.h>
 
-#include <functional>
-
 #include "sra.h"
 
 namespace sra {
@@ -33,7 +31,16 @@ sra_status forward_call(const sra_problem* p, const void* q_gen, const void* k_g
 // Sets the thread's last-error message and returns `s`.
 sra_status set_error(sra_status s, const char* msg);
 
-// Runs `launch` (kernel launches on `stream`), timed as kernel `kernel` where timing is on.
-hipError_t timed_launch(int kernel, hipStream_t stream, const std::function<hipError_t()>& launch);
+// Per-kernel timing of launches elsewhere: begin before them, end (with what begin gave) behind them, as kernel
+// `kernel`. Nothing is recorded while timing is off.
+hipEvent_t timing_begin(hipStream_t stream);
+void timing_end(int kernel, hipStream_t stream, hipEvent_t begin);
+template <class Launch>
+hipError_t timed_launch(int kernel, hipStream_t stream, Launch&& launch) {
+  const hipEvent_t begin = timing_begin(stream);
+  const hipError_t e = launch();
+  timing_end(kernel, stream, begin);
+  return e;
+}
 
 }  // namespace sra

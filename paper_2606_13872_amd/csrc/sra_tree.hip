@@ -96,6 +96,9 @@ __device__ __forceinline__ void tree_bounds(const TreeArgs& a, TreeBounds& s) {
     carry_first = __builtin_amdgcn_readlane(first, 63);
     carry_cost = __builtin_amdgcn_readlane(x, 63);
   }
+  // what a lane wrote, other lanes of the wave read: LDS keeps a wave's order, the compiler is to keep it too
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_wave_barrier();
 }
 
 // The sequence that cost position x belongs to: the first b with cost[b + 1] > x. Two looks of 64 lanes.
@@ -799,7 +802,7 @@ __global__ void __launch_bounds__(kTreeThreads) sra_append_kernel(AppendArgs a) 
   const PagedCache& c = a.c;
   const int lane = threadIdx.x & 63;
   const int i = __builtin_amdgcn_readfirstlane(blockIdx.x * kTreeWaves + (threadIdx.x >> 6));
-  if (i >= c.tokens) return;
+  if (uint32_t(i) >= uint32_t(c.tokens)) return;  // i of the last block may pass 31 bits
   // the sequence: as many end at or before token i
   int b = 0;
   for (int b0 = 0; b0 < c.batch; b0 += 64) {

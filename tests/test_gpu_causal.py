@@ -133,6 +133,28 @@ def test_empty_rows():
     assert bool((got["dq"][:70] == 0).all()) and bool((got["o"][90:] == 0).all())
 
 
+def test_no_tokens_and_no_keys():
+    print("causal nothing", flush=True)
+    got = _check([0], [70], 4, 2, 128)
+    assert got["o"].shape == (0, 4, 128) and bool((got["dk"] == 0).all()) and bool((got["dv"] == 0).all())
+    got = _check([3, 0], [0, 0], 4, 2, 64)
+    assert bool((got["lse"] == -float("inf")).all()) and bool((got["dq"] == 0).all()) and got["dk"].numel() == 0
+
+
+def test_kernel_timing_counts_the_launches():
+    print("causal timing", flush=True)
+    q, k, v, do = _inputs([300], [300], 4, 2, 64)
+    plan = sra.CausalPlan([300], 4, 2, 64)
+    sra.sra.kernel_timing_enable(True)
+    for _ in range(3):
+        o, lse = sra.causal_forward(q, k, v, plan)
+    sra.causal_backward(q, k, v, o, lse, do, plan)
+    t = sra.sra.kernel_timing()
+    sra.sra.kernel_timing_enable(False)
+    assert t["causal_forward"][1] == 3 and t["causal_delta"][1] == 1 and t["causal_grad"][1] == 1 and t["forward"][1] == 0
+    assert all(t[n][0] > 0 for n in ("causal_forward", "causal_delta", "causal_grad"))
+
+
 def test_repeats_are_bitwise_equal_and_buffers_are_used():
     print("causal repeats", flush=True)
     nq = [777, 130]
