@@ -12,7 +12,7 @@ from typing import Dict, Optional
 import numpy as np
 
 from . import sra as _s
-from .causal import _call, _no_alias
+from .causal import _addr, _call, _no_alias, _rows
 
 _declared = False
 
@@ -89,25 +89,6 @@ def _cache(k_cache, v_cache, page_table, context_lens, cu_tokens, tokens, kv_hea
         raise _s._bad("page_table: rows overlap")
     return _PagedCache(n, tokens, kv_heads, head_dim, shape[0], shape[1], width, _addr(k_cache), _addr(v_cache),
                        kp, vp, kt, vt, _addr(page_table), ts, _addr(context_lens), _addr(cu_tokens))
-
-
-def _addr(t):
-    return t.data_ptr() if t is not None and t.numel() else None
-
-
-def _rows(t, name, shape):
-    """Token stride of bf16 [tokens, heads, head_dim] with contiguous heads (0: at most one token)."""
-    torch = _s._tm()
-    if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16 or t.shape != shape:
-        _s._expect(t, name, shape, torch.bfloat16, False)  # says what is wrong
-    st = t.stride()
-    if shape[0] and (st[2] != 1 or (shape[1] > 1 and st[1] != shape[2])):
-        raise _s._bad(f"{name} must be [tokens, heads, head_dim] with contiguous heads")
-    if shape[0] <= 1:
-        return 0
-    if st[0] < shape[1] * shape[2]:
-        raise _s._bad(f"{name}: tokens overlap (stride {st[0]})")
-    return st[0]
 
 
 def _dims(t, name):

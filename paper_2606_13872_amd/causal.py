@@ -79,6 +79,9 @@ class CausalPlan:
         _s._check(L.sra_causal_plan_sizes(h, ctypes.byref(t), ctypes.byref(f), ctypes.byref(b)))
         self._table_bytes, self.forward_workspace, self.backward_workspace = t.value, f.value, b.value
         self.n_q, self.n_k = int(self.q_lens.sum(dtype=np.int64)), int(self.k_lens.sum(dtype=np.int64))
+        self.q_shape = (self.n_q, self.heads, self.head_dim)
+        self.k_shape = (self.n_k, self.kv_heads, self.head_dim)
+        self.lse_shape = (self.heads, self.n_q)
         self._tables = {}
         torch = _s._tm()
         if device is not None or torch.cuda.is_available():
@@ -103,7 +106,7 @@ class CausalPlan:
         t, home = self._tables.get(dev.index) or self._upload(dev.index)
         if stream.value != home and (stream.value or home):
             t.record_stream(_s._tm().cuda.current_stream(dev))
-        return ctypes.c_void_p(t.data_ptr())
+        return t.data_ptr()
 
     def mask(self, which: int, sequence: int, head: int) -> np.ndarray:
         """sra_causal_plan_mask: how often launch `which` (SCHED_*) computes each (token, key) pair."""
@@ -114,25 +117,29 @@ class CausalPlan:
         return out
 
 
-def _stride(t, name):
-    """Token stride of an input [tokens, heads, head_dim] with contiguous heads (0: it has at most one token)."""
-    if t.shape[0] <= 1:
+def _rows(t, name, shape):
+    """Checks an input, bf16 [tokens, heads, head_dim] with contiguous heads; its token stride (0: at most one token)."""
+    torch = _s._tm()
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16 or t.shape != shape:
+        _s._expect(t, name, shape, torch.bfloat16, False)  # says what is wrong
+    st = t.stride()
+    if shape[0] and (st[2] != 1 or (shape[1] > 1 and st[1] != shape[2])):
+        raise _s._bad(f"{name} must be [tokens, heads, head_dim] with contiguous heads")
+    if shape[0] <= 1:
         return 0
-    s = int(t.stride(0))
-    if s < t.shape[1] * t.shape[2]:
-        raise _s._bad(f"{name}: tokens overlap (stride {s})")
-    return s
+    if st[0] < shape[1] * shape[2]:
+        raise _s._bad(f"{name}: tokens overlap (stride {st[0]})")
+    return st[0]
+
+
+def _addr(t):
+    return t.data_ptr() if t is not None and t.numel() else None
 
 
 def _qkv(q, k, v, plan):
-    torch = _s._tm()
     if not isinstance(plan, CausalPlan):
         raise _s._bad("plan must be a CausalPlan")
-    bf = torch.bfloat16
-    _s._expect(q, "q", (plan.n_q, plan.heads, plan.head_dim), bf, False)
-    _s._expect(k, "k", (plan.n_k, plan.kv_heads, plan.head_dim), bf, False)
-    _s._expect(v, "v", (plan.n_k, plan.kv_heads, plan.head_dim), bf, False)
-    return _stride(q, "q"), _stride(k, "k"), _stride(v, "v")
+    return _rows(q, "q", plan.q_shape), _rows(k, "k", plan.k_shape), _rows(v, "v", plan.k_shape)
 
 
 def _no_alias(out, named):
@@ -169,19 +176,23 @@ def causal_forward(q, k, v, plan: CausalPlan, scale: Optional[float] = None, out
     """
     torch = _s._tm()
     qs, ks, vs = _qkv(q, k, v, plan)
-    o_shape, lse_shape = (plan.n_q, plan.heads, plan.head_dim), (plan.heads, plan.n_q)
-    _s._precheck_outs(out, [("o", o_shape, torch.bfloat16), ("lse", lse_shape, torch.float32)])
     dev = q.device
-    _s._same_device((("q", q), ("k", k), ("v", v)), dev)
-    out = out or {}
-    o = _s._out(out, "o", o_shape, torch.bfloat16, dev)
-    lse = _s._out(out, "lse", lse_shape, torch.float32, dev)
-    ws = _s._workspace(out, plan.forward_workspace, dev)
     if out:
+        _s._precheck_outs(out, [("o", plan.q_shape, torch.bfloat16), ("lse", plan.lse_shape, torch.float32)])
+    _s._same_device((("q", q), ("k", k), ("v", v)), dev)
+    need = plan.forward_workspace
+    if out:
+        o = _s._out(out, "o", plan.q_shape, torch.bfloat16, dev)
+        lse = _s._out(out, "lse", plan.lse_shape, torch.float32, dev)
+        ws = _s._workspace(out, need, dev)
         _no_alias(out, (("q", q), ("k", k), ("v", v), ("o", o), ("lse", lse), ("workspace", ws)))
+    else:
+        o = torch.empty(plan.q_shape, dtype=torch.bfloat16, device=dev)
+        lse = torch.empty(plan.lse_shape, dtype=torch.float32, device=dev)
+        ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
     _s._check(_call(dev, lambda s: _lib().sra_causal_forward(
-        plan._handle, plan._device_tables(dev, s), _s._ptr(q), _s._ptr(k), _s._ptr(v), qs, ks, vs, _s._ptr(o),
-        _s._ptr(lse), 0.0 if scale is None else float(scale), _s._ptr(ws), ws.numel(), s)))
+        plan._handle, plan._device_tables(dev, s), _addr(q), _addr(k), _addr(v), qs, ks, vs, _addr(o), _addr(lse),
+        0.0 if scale is None else float(scale), _addr(ws), 0 if ws is None else ws.numel(), s)))
     return o, lse
 
 
@@ -196,21 +207,25 @@ def causal_backward(q, k, v, o, lse, do, plan: CausalPlan, scale: Optional[float
     if not plan.backward:
         raise _s._bad("the plan was made with backward=False")
     bf = torch.bfloat16
-    q_shape, k_shape = (plan.n_q, plan.heads, plan.head_dim), (plan.n_k, plan.kv_heads, plan.head_dim)
-    _s._expect(o, "o", q_shape, bf, True)
-    _s._expect(do, "do", q_shape, bf, True)
-    _s._expect(lse, "lse", (plan.heads, plan.n_q), torch.float32, True)
-    _s._precheck_outs(out, [("dq", q_shape, bf), ("dk", k_shape, bf), ("dv", k_shape, bf)])
+    dense = (("o", o, plan.q_shape, bf), ("do", do, plan.q_shape, bf), ("lse", lse, plan.lse_shape, torch.float32))
+    for name, t, shape, dtype in dense:
+        _s._expect(t, name, shape, dtype, True)
     dev = q.device
-    _s._same_device((("q", q), ("k", k), ("v", v), ("o", o), ("lse", lse), ("do", do)), dev)
-    out = out or {}
-    g = {"dq": _s._out(out, "dq", q_shape, bf, dev), "dk": _s._out(out, "dk", k_shape, bf, dev),
-         "dv": _s._out(out, "dv", k_shape, bf, dev)}
-    ws = _s._workspace(out, plan.backward_workspace, dev)
+    grads = (("dq", plan.q_shape), ("dk", plan.k_shape), ("dv", plan.k_shape))
+    ins = (("q", q), ("k", k), ("v", v), ("o", o), ("lse", lse), ("do", do))
     if out:
-        _no_alias(out, (("q", q), ("k", k), ("v", v), ("o", o), ("lse", lse), ("do", do), *g.items(), ("workspace", ws)))
+        _s._precheck_outs(out, [(n, shape, bf) for n, shape in grads])
+    _s._same_device(ins, dev)
+    need = plan.backward_workspace
+    if out:
+        g = {n: _s._out(out, n, shape, bf, dev) for n, shape in grads}
+        ws = _s._workspace(out, need, dev)
+        _no_alias(out, ins + (*g.items(), ("workspace", ws)))
+    else:
+        g = {n: torch.empty(shape, dtype=bf, device=dev) for n, shape in grads}
+        ws = torch.empty(need, dtype=torch.uint8, device=dev) if need else None
     _s._check(_call(dev, lambda s: _lib().sra_causal_backward(
-        plan._handle, plan._device_tables(dev, s), _s._ptr(q), _s._ptr(k), _s._ptr(v), qs, ks, vs, _s._ptr(o),
-        _s._ptr(lse), _s._ptr(do), _s._ptr(g["dq"]), _s._ptr(g["dk"]), _s._ptr(g["dv"]),
-        0.0 if scale is None else float(scale), _s._ptr(ws), ws.numel(), s)))
+        plan._handle, plan._device_tables(dev, s), _addr(q), _addr(k), _addr(v), qs, ks, vs, _addr(o), _addr(lse),
+        _addr(do), _addr(g["dq"]), _addr(g["dk"]), _addr(g["dv"]), 0.0 if scale is None else float(scale), _addr(ws),
+        0 if ws is None else ws.numel(), s)))
     return g
