@@ -132,7 +132,7 @@ sra_status check_cache(const sra_paged_cache* c, bool pointers, bool tensors, Pa
   if (out->k_page < out->k_token * (c->page_size - 1) + row || out->v_page < out->v_token * (c->page_size - 1) + row ||
       out->k_page % 8 || out->v_page % 8)
     return fail(SRA_ERR_INVALID_ARGUMENT, "page strides must be multiples of 8 and hold a page");
-  if (out->k_page > (int64_t(1) << 40) || out->v_page > (int64_t(1) << 40))
+  if (out->k_page >= (int64_t(1) << 35) || out->v_page >= (int64_t(1) << 35))
     return fail(SRA_ERR_UNSUPPORTED, "a page stride is too large");
   out->table_stride = c->table_stride ? c->table_stride : c->max_pages;
   if (out->table_stride < c->max_pages) return fail(SRA_ERR_INVALID_ARGUMENT, "table_stride must be at least max_pages");
@@ -403,6 +403,8 @@ sra_status sra_tree_attention(const sra_paged_cache* c, int32_t num_heads, const
   a.heads = num_heads;
   const uint32_t G = uint32_t(num_heads / c->num_kv_heads);
   a.group_magic = G > 1 ? uint32_t((uint64_t(1) << 32) / G + 1) : 0;
+  a.k_step = {uint32_t(a.c.k_page / 8), uint32_t(a.c.k_token / 8)};
+  a.v_step = {uint32_t(a.c.v_page / 8), uint32_t(a.c.v_token / 8)};
   a.scale_log2 = float(double(scale_of(softmax_scale, c->head_dim)) * 1.4426950408889634);
   a.part = static_cast<float*>(workspace);
   a.split = reinterpret_cast<TreeSplit*>(static_cast<char*>(workspace) + tree_slots_bytes(rows, c->head_dim));

@@ -61,6 +61,12 @@ SRA_HD inline int64_t append_position(const PagedCache& c, int32_t b, int32_t i)
   return i < first ? -1 : pos - first;
 }
 
+// 8-element (16-byte) strides in 32 bits, for the scalar address arithmetic of the tree kernels' loads: a page holds less
+// than 2^35 elements.
+struct PageSteps {
+  uint32_t page, token;
+};
+
 struct TreeArgs {
   PagedCache c;
   const __bf16 *q, *k, *v;  // [tokens, heads, D], [tokens, kv_heads, D]
@@ -70,6 +76,7 @@ struct TreeArgs {
   float* lse;               // [heads, tokens]
   int32_t heads;
   uint32_t group_magic;     // ceil(2^32 / G), for exact divisions of small numbers by G = heads / kv_heads > 1
+  PageSteps k_step, v_step;
   float scale_log2;
   float* part;              // [2 kTreeGroups] slots: O [rows, D], then (m, l) per row (rows per group of rows)
   TreeSplit* split;         // [kTreeGroups]

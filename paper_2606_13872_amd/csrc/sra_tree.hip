@@ -180,6 +180,11 @@ __device__ __forceinline__ uint64_t lane_u64(uint64_t x, int lane) {
   return (uint64_t(hi) << 32) | lo;
 }
 
+// Address of slot `slot` of page `id`.
+__device__ __forceinline__ uint64_t page_row(uint64_t base, const PageSteps& s, int id, int slot) {
+  return base + ((uint64_t(uint32_t(id)) * s.page + uint32_t(slot) * s.token) << 4);
+}
+
 // Per-wave state of a run over one group of rows.
 template <int D, int NQ>
 struct TreeState {
@@ -338,6 +343,8 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
     if (c0 >= c1) continue;  // the run ends before the group's first chunk
     const const_ints table = (const_ints)(uintptr_t)(c.table + int64_t(seg.b) * c.table_stride);
 
+    const uint64_t kbase = uniform_u64(reinterpret_cast<uint64_t>(c.k + int64_t(seg.kvh) * D));
+    const uint64_t vbase = uniform_u64(reinterpret_cast<uint64_t>(c.v + int64_t(seg.kvh) * D));
     // Page ids of chunk i's four groups of 8 rows (a page holds a multiple of 8), where the chunk is all context.
     struct Ids {
       int v[4];
@@ -362,15 +369,13 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
           constexpr int kPer = kInstr / 4;  // load instructions of 8 rows
 #pragma unroll
           for (int kv = 0; kv < 2; ++kv) {
-            const __bf16* base = (kv ? c.v : c.k) + int64_t(seg.kvh) * D;
-            const int64_t ps = kv ? c.v_page : c.k_page, ts = kv ? c.v_token : c.k_token;
-            const uint32_t lane_row = uint32_t(lrow * ts);
+            const PageSteps step = kv ? a.v_step : a.k_step;
+            const uint32_t lane_row = lrow * step.token * 16;
 #pragma unroll
             for (int j = 0; j < kInstr; ++j) {
-              const int slot = (p0 + (j / kPer) * 8) & (page_rows - 1);
-              const __bf16* src = base + ids.v[j / kPer] * ps + slot * ts + (j % kPer) * (RPI * ts);
-              lds_dma_x4_off(uniform_u64(reinterpret_cast<uint64_t>(src)), (lane_row + chunk16[j % kKinds]) * 2,
-                             la + kv * kTile + j * 1024);
+              const int slot = ((p0 + (j / kPer) * 8) & (page_rows - 1)) + (j % kPer) * RPI;
+              lds_dma_x4_off(uniform_u64(page_row(kv ? vbase : kbase, step, ids.v[j / kPer], slot)),
+                             lane_row + chunk16[j % kKinds] * 2, la + kv * kTile + j * 1024);
             }
           }
           return ~0u;
@@ -600,8 +605,8 @@ sra_tree_shared_kernel(TreeArgs a) {
 #pragma unroll
       for (int j = 0; j < kPer; ++j) {
         const int slot = (i * C + RPI * (wave + j * kWaves)) & page_mask;
-        const int64_t row = ids.v[j] * (is_v ? c.v_page : c.k_page) + slot * (is_v ? c.v_token : c.k_token);
-        lds_dma_x4_off(uniform_u64((is_v ? vbase : kbase) + uint64_t(row) * 2), is_v ? voff : koff, la + j * kWaves * 1024);
+        lds_dma_x4_off(uniform_u64(page_row(is_v ? vbase : kbase, is_v ? a.v_step : a.k_step, ids.v[j], slot)),
+                       is_v ? voff : koff, la + j * kWaves * 1024);
       }
     };
     int next_k = c0, next_v = c0;
