@@ -260,8 +260,9 @@ sra_status sra_launch_export(const sra_problem* p, int which, int32_t* items, in
  *             host: what a call does for bad ones is stated there, and no such value makes it read or write
  *             outside the tensors it was given.
  *   Rows that see no key have o = 0, lse = -inf and no part in any gradient. So have rows whose scores are all
- *             -inf. An infinity or NaN in v reaches, as in a product with zeros, also rows of its sequence that
- *             do not see the key, never another sequence's.                                                  */
+ *             -inf. An infinity or NaN in v (the gradients: in any input) reaches, as in a product with zeros,
+ *             also rows and keys of its sequence that the mask keeps apart from it, never another sequence's.
+ *   Devices   a call launches on the current device, which must be the stream's.                             */
 
 /* Lengths of packed sequences (host memory, read by sra_causal_plan_create only). */
 typedef struct sra_causal_problem {
@@ -281,7 +282,9 @@ typedef struct sra_causal_plan sra_causal_plan;
 /* Plans causal attention (§2.3) of packed sequences: token i of a sequence with nq tokens and nk keys sees the keys
  * j <= i + nk - nq, so the last token sees the last key (nk > nq: the sequence continues earlier keys; with
  * nq > nk the first nq - nk tokens see nothing). backward != 0 plans the gradients too.
- * Host only. num_heads * tokens and num_kv_heads * keys <= 2^31 - 1 (beyond: SRA_ERR_UNSUPPORTED). */
+ * Host only. num_heads * tokens and num_kv_heads * keys are below 2^28, and there are at most 2^22 / num_kv_heads
+ * blocks of 256 keys, and of 256 (token, query head of a K/V head) pairs, of a sequence each (beyond:
+ * SRA_ERR_UNSUPPORTED). */
 sra_status sra_causal_plan_create(const sra_causal_problem* p, int backward, sra_causal_plan** plan);
 
 /* Library infrastructure: frees a plan (NULL is allowed). Calls that were enqueued with it do not need it any more, only
@@ -325,11 +328,11 @@ sra_status sra_causal_backward(const sra_causal_plan* plan, const void* tables, 
  * page_table, context_lens and cu_tokens are DEVICE arrays, read when the call runs: a captured call serves any
  * values. Sequence b holds context_lens[b] cached positions (taken as 0 below 0, and as max_pages * page_size
  * above that) and the new tokens cu_tokens[b] .. cu_tokens[b + 1] - 1 of the packed ones (clamped to [0, tokens];
- * sra_tree_attention also takes a falling entry as equal to the one before). Tokens behind the last sequence's
- * are padding: their outputs are left as they were. */
+ * sra_tree_attention also takes a falling entry as equal to the one before). Tokens before the first sequence's and
+ * behind the last one's are padding: their outputs are left as they were. */
 typedef struct sra_paged_cache {
   int32_t batch;              /* sequences, 1 .. 2048                                       */
-  int32_t tokens;             /* rows of the packed new tokens, >= 0                        */
+  int32_t tokens;             /* rows of the packed new tokens, 0 .. 2^25                   */
   int32_t num_kv_heads;
   int32_t head_dim;           /* 64 or 128                                                  */
   int32_t num_pages;          /* >= 1                                                       */
@@ -337,7 +340,7 @@ typedef struct sra_paged_cache {
   int32_t max_pages;          /* entries of a page_table row, >= 1; max_pages * page_size <= 2^30 */
   void* k;
   void* v;
-  int64_t k_page_stride, v_page_stride;    /* elements; 0 selects page_size * token stride  */
+  int64_t k_page_stride, v_page_stride;    /* elements, < 2^35; 0 selects page_size * token stride */
   int64_t k_token_stride, v_token_stride;  /* elements; 0 selects num_kv_heads * head_dim   */
   const int32_t* page_table;
   int64_t table_stride;       /* entries between rows, >= max_pages; 0 selects max_pages    */
@@ -357,8 +360,9 @@ sra_status sra_tree_workspace_size(const sra_paged_cache* c, int32_t num_heads, 
  *   is set, and later tokens of a longer sequence are seen by none. NULL: a chain of any length, each token sees the
  *   new tokens of its sequence up to itself.
  * Positions of pages whose id is not in [0, num_pages) are seen by no token.
- * Deterministic; enqueues kernels only. The order of sums follows all lengths of the call. workspace: 256-byte aligned,
- * as sra_tree_workspace_size says, no initialisation; calls that may overlap need one each. */
+ * At most 1024 query heads per K/V head. Deterministic; enqueues kernels only. The order of sums follows all lengths of
+ * the call. workspace: 256-byte aligned, as sra_tree_workspace_size says, no initialisation; calls that may overlap
+ * need one each. */
 sra_status sra_tree_attention(const sra_paged_cache* c, int32_t num_heads, const void* q, const void* k,
                               const void* v, int64_t q_stride, int64_t k_stride, int64_t v_stride,
                               const uint64_t* tree, void* o, float* lse, float softmax_scale, void* workspace,
@@ -370,7 +374,8 @@ sra_status sra_tree_attention(const sra_paged_cache* c, int32_t num_heads, const
  * n_rows = tokens). context_lens is not changed: the caller adds the tokens' number when it wants them seen.
  * Tokens whose position lies behind the page_table row or in a page whose id is not in [0, num_pages), or whose row
  * is not in [0, n_rows), are skipped. Two tokens of a call never share a position of a sequence; where page_table
- * names a page twice, which of its writers' rows a slot ends up with is not defined. */
+ * names a page twice, which of its writers' rows a slot ends up with is not defined. No row of the k pages shares memory
+ * with one of the v pages, nor with k or v. */
 sra_status sra_cache_append(const sra_paged_cache* c, const void* k, const void* v, int64_t k_stride,
                             int64_t v_stride, const int32_t* rows, int32_t n_rows, void* stream);
 

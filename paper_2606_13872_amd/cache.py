@@ -91,6 +91,24 @@ def _cache(k_cache, v_cache, page_table, context_lens, cu_tokens, tokens, kv_hea
                        kp, vp, kt, vt, _addr(page_table), ts, _addr(context_lens), _addr(cu_tokens))
 
 
+def _rows_apart(c, row):
+    """Whether no K row of the cache shares memory with a V row (both are written at once): the tensors lie apart, or have
+    the same strides and the V rows lie between the K pages, or between their tokens."""
+    def end(page, token):
+        return 2 * ((c.num_pages - 1) * page + (c.page_size - 1) * token + row)
+    d = (c.v or 0) - (c.k or 0)
+    if d >= end(c.k_page_stride, c.k_token_stride) or -d >= end(c.v_page_stride, c.v_token_stride):
+        return True
+    page, token = c.k_page_stride, c.k_token_stride
+    if (c.v_token_stride, c.num_pages > 1 and c.v_page_stride) != (token, c.num_pages > 1 and page) or d % 2:
+        return False
+    d //= 2
+    span = (c.page_size - 1) * token + row
+    if c.num_pages > 1 and span <= d % page <= page - span:
+        return True
+    return (c.num_pages == 1 or page % token == 0) and row <= d % token <= token - row
+
+
 def _dims(t, name):
     if not isinstance(t, _s._tm().Tensor) or t.dim() != 3:
         raise _s._bad(f"{name} must be a [tokens, heads, head_dim] tensor")
@@ -109,7 +127,8 @@ def tree_attention(q, k, v, k_cache, v_cache, page_table, context_lens, cu_token
     tree: int64 [tokens], bit j of token i's mask = it sees new token j (< 64) of its sequence, itself included only
     if its own bit is set. None: each token sees the new tokens of its sequence up to itself (a single token, or a chain
     of any length).
-    o: bf16 like q, dense; lse fp32 [heads, tokens]. Tokens behind cu_tokens[-1] are padding and keep what `out` held.
+    o: bf16 like q, dense; lse fp32 [heads, tokens]. Tokens that are no sequence's (before cu_tokens[0], behind
+    cu_tokens[-1]) are padding and keep what `out` held.
     Positions in pages outside the cache are seen by no token. `out` may hold o, lse and workspace (uint8).
     """
     torch = _s._tm()
@@ -167,8 +186,8 @@ def cache_append(k, v, k_cache, v_cache, page_table, context_lens, cu_tokens, ro
 
     k, v: bf16 [n, kv_heads, head_dim]; without `rows` their rows are the packed tokens. rows: int32 [tokens], the row
     of k and v that each packed token is (the accepted tokens of a drafted tree). Cache, page_table, context_lens and
-    cu_tokens as for tree_attention. Tokens behind the page_table row, in a page outside the cache or with a row outside
-    k and v are skipped.
+    cu_tokens as for tree_attention; k_cache and v_cache must not share rows. Tokens behind the page_table row, in a page
+    outside the cache or with a row outside k and v are skipped.
     """
     n, kv, d = _dims(k, "k")
     ks, vs = _rows(k, "k", (n, kv, d)), _rows(v, "v", (n, kv, d))
@@ -178,6 +197,8 @@ def cache_append(k, v, k_cache, v_cache, page_table, context_lens, cu_tokens, ro
         tokens = rows.shape[0]
     c = _cache(k_cache, v_cache, page_table, context_lens, cu_tokens, tokens, kv, d)
     dev = k.device
+    if not _rows_apart(c, kv * d):
+        raise _s._bad("k_cache and v_cache overlap")
     if n and c.num_pages:  # rows are read while others are written
         spans = [(t.data_ptr(), t.data_ptr() + 2 * ((t.shape[0] - 1) * s + kv * d)) for t, s in ((k, ks), (v, vs))]
         for cache, ps, ts in ((k_cache, c.k_page_stride, c.k_token_stride), (v_cache, c.v_page_stride, c.v_token_stride)):

@@ -56,6 +56,7 @@ def _lens(x, name) -> np.ndarray:
 class CausalPlan:
     """The tile schedule of causal attention for one set of lengths, with its tables on `device` (default: the
     current GPU; without a GPU only the host hooks work). Made once, used by every layer and call with these lengths.
+    A plan is made outside a graph's capture, and kept as long as graphs that hold calls with it (they read its tables).
 
     q_lens: tokens of each packed sequence. k_lens: its keys, where they differ (the sequence continues earlier
     keys: token i of nq sees the keys j <= i + nk - nq). backward=False plans the forward alone.
@@ -93,6 +94,8 @@ class CausalPlan:
     def _upload(self, index: int):
         """The tables on GPU `index` (its address and the stream that they were copied on)."""
         torch = _s._tm()
+        if torch.cuda.is_current_stream_capturing():
+            raise _s._bad(f"the plan's tables are not on GPU {index}: make the plan, for this GPU, before the capture")
         host = np.zeros(max(1, self._table_bytes), dtype=np.uint8)
         _s._check(_lib().sra_causal_plan_tables(self._handle, host.ctypes.data, self._table_bytes))
         with torch.cuda.device(index):

@@ -26,6 +26,11 @@ using namespace sra;
 constexpr size_t kAlign = 256;
 constexpr int64_t kMaxInt = 2147483647;
 constexpr int64_t kMaxStride = kMaxInt / 64;  // offsets inside a tile are 32-bit
+// A launch has less than 2^32 threads: the delta kernel takes up to 16 for a (token, head) pair, the items 256 or 512
+// each, the append 64 a token.
+constexpr int64_t kMaxPairs = (int64_t(1) << 28) - 1;
+constexpr int64_t kMaxItems = int64_t(1) << 22;
+constexpr int32_t kMaxTokens = 1 << 25;
 
 size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 sra_status fail(sra_status s, const std::string& msg) { return set_error(s, msg.c_str()); }
@@ -119,6 +124,7 @@ sra_status check_cache(const sra_paged_cache* c, bool pointers, bool tensors, Pa
     return fail(SRA_ERR_INVALID_ARGUMENT, "page_size must be a power of two of at least 8");
   if (int64_t(c->max_pages) * c->page_size > (int64_t(1) << 30))
     return fail(SRA_ERR_UNSUPPORTED, "max_pages * page_size must be at most 2^30");
+  if (c->tokens > kMaxTokens) return fail(SRA_ERR_UNSUPPORTED, "tokens must be at most " + std::to_string(kMaxTokens));
   if (int64_t(c->tokens) * c->num_kv_heads > kMaxInt) return fail(SRA_ERR_UNSUPPORTED, "heads * tokens must be below 2^31");
   out->k = static_cast<__bf16*>(c->k);
   out->v = static_cast<__bf16*>(c->v);
@@ -199,16 +205,23 @@ sra_status sra_causal_plan_create(const sra_causal_problem* p, int backward, sra
     t.kv_heads = p->num_kv_heads;
     t.head_dim = p->head_dim;
     t.backward = backward != 0;
+    if (int64_t(t.heads) * t.head_dim > kMaxStride) return fail(SRA_ERR_UNSUPPORTED, "too many heads");
     const int32_t* k_lens = p->k_lens ? p->k_lens : p->q_lens;
-    for (int32_t b = 0; b < p->batch; ++b) {
+    for (int32_t b = 0; b < p->batch; ++b)
       if (p->q_lens[b] < 0 || k_lens[b] < 0) return fail(SRA_ERR_INVALID_ARGUMENT, "lengths must not be negative");
+    const int64_t G = t.heads / t.kv_heads;
+    int64_t q_items = 0, k_items = 0;
+    for (int32_t b = 0; b < p->batch; ++b) {
       t.nq.push_back(p->q_lens[b]);
       t.nk.push_back(k_lens[b]);
       t.q_rows += p->q_lens[b];
       t.k_rows += k_lens[b];
+      if (t.q_rows * t.heads > kMaxPairs || t.k_rows * t.kv_heads > kMaxPairs)
+        return fail(SRA_ERR_UNSUPPORTED, "heads * packed tokens must be below 2^28");
+      q_items += (p->q_lens[b] * G + kCausalTile - 1) / kCausalTile * t.kv_heads;
+      k_items += (int64_t(k_lens[b]) + kCausalTile - 1) / kCausalTile * t.kv_heads;
+      if (q_items > kMaxItems || k_items > kMaxItems) return fail(SRA_ERR_UNSUPPORTED, "too many sequences times K/V heads");
     }
-    if (t.q_rows * t.heads > kMaxInt || t.k_rows * t.kv_heads > kMaxInt)
-      return fail(SRA_ERR_UNSUPPORTED, "heads * packed tokens must be below 2^31");
     build_causal_tables(&t);
     size_t at = 0;
     for (int i = 0; i < 4; ++i) {

@@ -175,3 +175,36 @@ def test_library_refuses_before_any_launch():
     n = ctypes.c_size_t()
     assert L.sra_tree_workspace_size(ctypes.byref(paged(k=null, page_table=null)), 4, ctypes.byref(n)) == 0 and n.value % 256 == 0
     assert L.sra_tree_workspace_size(ctypes.byref(paged()), 4, null) == 1
+
+
+@pytest.mark.parametrize("apart,layout", [
+    (True, lambda x: (x[0, :, 0], x[1, :, 0])),              # two buffers
+    (True, lambda x: (x[0, :, 0], x[0, :, 1])),              # K and V pages in turn
+    (True, lambda x: (x[0, :, 1], x[0, :, 0])),
+    (True, lambda x: (x[0].view(4, 16, 2, 2, 64)[:, :, 0], x[0].view(4, 16, 2, 2, 64)[:, :, 1])),  # tokens in turn
+    (True, lambda x: (x[0, :1, 0], x[0, :1, 1])),            # one page
+    (False, lambda x: (x[0, :, 0], x[0, :, 0])),             # the same one
+    (False, lambda x: (x[0].flatten(0, 1)[:4], x[0].flatten(0, 1)[1:5])),  # a page further
+    (False, lambda x: (x[0, :, 0], x[0].flatten(0, 1)[1:5])),  # other strides
+    (False, lambda x: (x[0, :1, 0], x.view(-1)[128:128 + 2048].view(1, 16, 2, 64))),  # a token further
+])
+def test_an_append_needs_its_own_rows_for_keys_and_values(apart, layout):
+    k, v = layout(torch.zeros(2, 4, 2, 16, 2, 64, dtype=torch.bfloat16))
+    new = torch.zeros(3, 2, 64, dtype=torch.bfloat16)
+    c = binding._cache(k, v, torch.tensor([[0]], dtype=I32), torch.tensor([1], dtype=I32), torch.tensor([0, 3], dtype=I32),
+                       3, 2, 64)
+    assert binding._rows_apart(c, 128) == apart
+    if not apart:
+        with pytest.raises(sra.SRAError, match="overlap"):
+            sra.cache_append(new, new.clone(), k, v, torch.tensor([[0]], dtype=I32), torch.tensor([1], dtype=I32),
+                             torch.tensor([0, 3], dtype=I32))
+
+
+def test_more_tokens_than_a_launch_takes_are_refused():
+    k = torch.zeros(1, 1, 64, dtype=torch.bfloat16).expand(2**25 + 1, 1, 64)
+    c = cache(kv=1)
+    args = (torch.tensor([[0]], dtype=I32), torch.tensor([1], dtype=I32), torch.tensor([0, 3], dtype=I32))
+    paged = binding._cache(c, c, *args, k.shape[0], 1, 64)
+    with pytest.raises(sra.SRAError) as e:
+        binding._workspace_size(paged, 1)
+    assert e.value.status == 2

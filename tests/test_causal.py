@@ -161,3 +161,20 @@ def test_library_refuses_before_any_launch():
     assert L.sra_causal_plan_tables(h, null, plan._table_bytes) == 1
     assert L.sra_causal_plan_mask(h, 7, 0, 0, fake) == 1 and L.sra_causal_plan_mask(h, 0, 1, 0, fake) == 1
     assert L.sra_causal_plan_destroy(null) == 0
+
+
+@pytest.mark.parametrize("args", [
+    dict(q_lens=[2**28], heads=1, kv_heads=1, head_dim=64), dict(q_lens=[1], k_lens=[2**24], heads=32, kv_heads=16, head_dim=64),
+    dict(q_lens=[2**31 - 1] * 4, heads=2**30, kv_heads=2**30, head_dim=64),  # their product passes 64 bits
+    dict(q_lens=[0], heads=2**24, kv_heads=1, head_dim=64), dict(q_lens=[0, 1] * 2**15, heads=256, kv_heads=256, head_dim=128),
+])
+def test_sizes_past_what_a_launch_takes_are_refused(args):
+    with pytest.raises(sra.SRAError) as e:
+        sra.CausalPlan(**args)
+    assert e.value.status == 2
+
+
+def test_largest_plans():
+    p = sra.CausalPlan([1], 1, 1, 64, k_lens=[2**28 - 1])
+    assert p.n_k == 2**28 - 1 and p.backward_workspace > 0
+    assert sra.CausalPlan([2**18 - 1], 1, 1, 128, k_lens=[1], backward=False).n_q == 2**18 - 1

@@ -241,3 +241,11 @@ def test_two_streams_at_once():
         assert torch.equal(a[0], o) and torch.equal(a[1], lse)
         for n in g:
             assert torch.equal(g[n], want[n]), n
+
+
+def test_plans_are_made_outside_a_capture():
+    x = torch.zeros(1, device="cuda")
+    with torch.cuda.graph(torch.cuda.CUDAGraph()):
+        with pytest.raises(sra.SRAError, match="capture"):
+            sra.CausalPlan([5], 4, 2, 64)
+        x.add_(1)
