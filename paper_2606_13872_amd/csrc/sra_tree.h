@@ -12,6 +12,14 @@ constexpr int kTreeGroups = 256;     // workgroups of a launch: one per compute 
 // waves are a chain of latencies (about 5 us, the time of as many chunks of four waves when the cache bounds them).
 constexpr int kTreeStart = 8;
 constexpr int kTreeMinRun = kTreeStart + 8;  // a workgroup takes at least so much: two chunks per wave
+// The same of the shared kernel, where a 64-key chunk costs 3 with up to 128 rows (1.9 us) and 4 with
+// more (2.5 us in long launches). Trees of up to 48 tokens over 16 contexts take 70 us for 67 with a start of 16 or 33; 16
+// requests of 1,000 positions and 10 tokens 29 us for 26 with a least run of 48.
+constexpr int kSharedStart = 24, kSharedMinRun = 36, kSharedNarrow = 3, kSharedWide = 4;
+// Launches whose runs of wide groups (256 rows) would cost less than this are dealt as narrow ones (128): more groups, so
+// fewer are split, for reading the keys of sequences with more rows again. 16 requests of 64 tokens x 4 heads: over 1,000
+// positions 37 us for 50, over 8,000 184 for 167.
+constexpr int kSharedShortRun = 120;
 constexpr int kTreeMaxGroup = 1024;          // query heads of a K/V head
 
 #ifndef SRA_HD

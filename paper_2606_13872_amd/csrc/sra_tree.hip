@@ -2,10 +2,10 @@
 //
 // Every new token of a sequence sees the sequence's whole cached context and, of the sequence's new tokens, those
 // that its tree mask names; one softmax over both. The G query heads of a K/V head are taken together: "rows" are
-// (token, head of the group) pairs, 16 NQ of them to a group of rows, so that K and V are read once for all of them.
+// (token, head of the group) pairs, 16 to 256 of them to a group of rows, so that K and V are read once for all of them.
 //
-// Bound by reading the cache: all of the launch's keys, counted in 32-key chunks (of each sequence, K/V head and
-// group of rows, one after the other, with kTreeStart more for beginning each group), are dealt to the workgroups in
+// Bound by reading the cache: all of the launch's keys, counted in chunks of 32 or 64 (of each sequence, K/V head and
+// group of rows, one after the other, with kStart more for beginning each group), are dealt to the workgroups in
 // equal runs, whatever the lengths; a run may end one group of rows and begin another. Lengths are read on the
 // device, so a captured call serves any lengths. A group that several workgroups share is added up by a second
 // kernel, in the order of its keys.
@@ -19,9 +19,9 @@
 // TB/s of algorithmic bytes, no other bytes fetched; two of 120 to 131 thousand 191 us (5.4 TB/s); four of 31 to 1,500
 // 12 us, a chain of latencies: launch, bounds 1.2 us, first loads 2.5, two chunks 2.5, merge 1, and another 4 us for the
 // second kernel. 64 head dims read 4.4 TB/s (half as long rows); from a cache of a few pages (L2) the kernel takes half
-// the time. Trees of up to 48 tokens over 16 contexts, 40 query heads: 85 us (each row group alone with its keys,
-// 226 us; shared tiles without the software pipeline, 125 us); 64 tokens each over 16 x 16,384 positions 325 us,
-// 845 TFLOP/s.
+// the time. Trees of up to 48 tokens over 16 contexts, 40 query heads, both kernels: 68 us (each 32 rows alone
+// with their keys 226, shared tiles without the software pipeline 125, 256 rows to every group 80); 64 tokens each over
+// 16 x 16,384 positions 307 us, 890 TFLOP/s.
 #include "sra_fwd_pipe.h"
 #include "sra_tree.h"
 
@@ -31,6 +31,12 @@ namespace {
 constexpr int kTreeWaves = 4;
 constexpr int kTreeThreads = kTreeWaves * 64;
 constexpr int kSharedChunk = 64;
+constexpr int kNarrow = 128;  // rows of a narrow group of the shared kernel: 16 per wave
+// Costs by C, the keys of a chunk: of beginning a group, of a chunk of a narrow and of a wide group, and of the least run.
+template <int C> constexpr int kStart = C == kSharedChunk ? kSharedStart : kTreeStart;
+template <int C> constexpr int kNarrowCost = C == kSharedChunk ? kSharedNarrow : 1;
+template <int C> constexpr int kWideCost = C == kSharedChunk ? kSharedWide : 1;
+template <int C> constexpr int kMinRun = C == kSharedChunk ? kSharedMinRun : kTreeMinRun;
 template <int D> constexpr int kStages = D == 128 ? 2 : 4;  // chunks of a wave's ring: 32 KB
 typedef const __attribute__((address_space(4))) int32_t* const_ints;  // read by scalar loads
 }  // namespace
@@ -58,23 +64,40 @@ __device__ __forceinline__ int wave_scan(int x, int none, F f) {
 // Bounds of the sequences: first[b] .. first[b + 1] are b's tokens (cu_tokens clamped into [0, tokens] and never
 // falling, so no token has two sequences), ctx[b] its cached positions, cost[b] .. cost[b + 1] the costs, in chunks, of
 // its groups of rows of all K/V heads.
+template <int kDeals>
 struct TreeBounds {
   int32_t first[kTreeMaxBatch + 1];
-  int32_t cost[kTreeMaxBatch + 1];
   int32_t ctx[kTreeMaxBatch];
+  int32_t cost[kDeals][kTreeMaxBatch + 1];
 };
+
+// The cost of a group of rows with n chunks, and of a sequence's groups of R rows (the last may hold fewer).
+template <int C>
+__device__ __forceinline__ int chunk_cost(int rows) {
+  return rows > kNarrow ? kWideCost<C> : kNarrowCost<C>;
+}
+template <int C>
+__device__ __forceinline__ int group_cost(int rows, int n) {
+  return kStart<C> + n * chunk_cost<C>(rows);
+}
+template <int C>
+__device__ __forceinline__ int groups_cost(int rows, int n, int R) {
+  const int whole = (rows - 1) / R;
+  return whole * group_cost<C>(R, n) + group_cost<C>(rows - whole * R, n);
+}
 
 __device__ __forceinline__ int group_div(const TreeArgs& a, int G, int x) {  // x / G, x < G + 256
   return G == 1 ? x : int(__umulhi(uint32_t(x), a.group_magic));
 }
 
-// Every wave fills all of s, with the same values, so none waits for another. R rows to a group, C keys to a chunk.
-template <int R, int C>
-__device__ __forceinline__ void tree_bounds(const TreeArgs& a, TreeBounds& s) {
+// Every wave fills all of s, with the same values, so none waits for another. Deal e has groups of R >> e rows; C keys to
+// a chunk.
+template <int R, int C, int kDeals>
+__device__ __forceinline__ void tree_bounds(const TreeArgs& a, TreeBounds<kDeals>& s) {
   const int lane = threadIdx.x & 63, n = a.c.batch;
   const int G = a.heads / a.c.kv_heads;
-  int carry_first = 0, carry_cost = 0;
-  if (lane == 0) s.cost[0] = 0;
+  int carry_first = 0, carry_cost[kDeals] = {};
+  if (lane < kDeals) s.cost[lane][0] = 0;
   int f = 0, end = 0, ctx = 0;
   auto read = [&](int b) {
     f = end = ctx = 0;
@@ -93,17 +116,20 @@ __device__ __forceinline__ void tree_bounds(const TreeArgs& a, TreeBounds& s) {
     read(b + 64);  // the next ones, on their way during the scans
     first = max(carry_first, wave_scan(first, 0, [](int x, int y) { return max(x, y); }));
     const int t = max(first, last) - first;
-    const int chunks = kTreeStart + (cached + t + C - 1) / C;
-    int x = b < n && t > 0 ? chunks * ((t * G + R - 1) / R) * a.c.kv_heads : 0;
-    x = carry_cost + wave_scan(x, 0, [](int x, int y) { return x + y; });
+    const int chunks = (cached + t + C - 1) / C;
+#pragma unroll
+    for (int e = 0; e < kDeals; ++e) {
+      int x = b < n && t > 0 ? groups_cost<C>(t * G, chunks, R >> e) * a.c.kv_heads : 0;
+      x = carry_cost[e] + wave_scan(x, 0, [](int x, int y) { return x + y; });
+      if (b < n) s.cost[e][b + 1] = x;
+      carry_cost[e] = __builtin_amdgcn_readlane(x, 63);
+    }
     if (b < n) {
       s.first[b] = first;
       s.ctx[b] = cached;
-      s.cost[b + 1] = x;
       if (b == n - 1) s.first[n] = first + t;
     }
     carry_first = __builtin_amdgcn_readlane(first, 63);
-    carry_cost = __builtin_amdgcn_readlane(x, 63);
   }
   // what a lane wrote, other lanes of the wave read: LDS keeps a wave's order, the compiler is to keep it too
   asm volatile("" ::: "memory");
@@ -111,11 +137,11 @@ __device__ __forceinline__ void tree_bounds(const TreeArgs& a, TreeBounds& s) {
 }
 
 // The sequence that cost position x belongs to: the first b with cost[b + 1] > x. Two looks of 64 lanes.
-__device__ __forceinline__ int tree_sequence(const TreeBounds& s, int n, int x) {
+__device__ __forceinline__ int tree_sequence(const int32_t* cost, int n, int x) {
   const int lane = threadIdx.x & 63, step = (n + 63) >> 6;
   auto look = [&](int b, int by, bool in) {  // how many of cost[b + by], cost[b + 2 by], .. (b + 64 by at most) x is past
     const int e = b + (lane + 1) * by;
-    return __builtin_popcountll(__builtin_amdgcn_ballot_w64(in && e <= n && s.cost[min(e, n)] <= x));
+    return __builtin_popcountll(__builtin_amdgcn_ballot_w64(in && e <= n && cost[min(e, n)] <= x));
   };
   const int b = step * look(0, step, true);
   return step == 1 ? b : b + look(b, 1, lane < step);
@@ -126,24 +152,31 @@ struct TreeSegment {
   int b, t0, t, ctx;   // sequence, first token, tokens, cached positions
   int kvh, row0, rows;
   int n, c0, c1;       // chunks of the group, and of this run
-  int origin;          // cost position of the group's first chunk
+  int origin, chunk;   // cost position of the group's first chunk, cost of a chunk
+  __device__ __forceinline__ int behind() const { return origin + n * chunk; }
+  // Runs that have chunks of the group, from its first chunk's, w, on.
+  __device__ __forceinline__ int pieces(int w, int run) const { return (origin + (n - 1) * chunk) / run - w + 1; }
 };
-template <int R, int C>
-__device__ __forceinline__ TreeSegment tree_segment(const TreeArgs& a, const TreeBounds& s, int G, int x, int end) {
+template <int C, int kDeals>
+__device__ __forceinline__ TreeSegment tree_segment(const TreeArgs& a, const TreeBounds<kDeals>& s, int deal, int R, int G,
+                                                    int x, int end) {
   TreeSegment g;
-  g.b = __builtin_amdgcn_readfirstlane(tree_sequence(s, a.c.batch, x));
+  g.b = __builtin_amdgcn_readfirstlane(tree_sequence(s.cost[deal], a.c.batch, x));
   g.t0 = __builtin_amdgcn_readfirstlane(s.first[g.b]);
   g.t = __builtin_amdgcn_readfirstlane(s.first[g.b + 1]) - g.t0;
   g.ctx = __builtin_amdgcn_readfirstlane(s.ctx[g.b]);
   g.n = (g.ctx + g.t + C - 1) / C;  // keys: the context's, then the new tokens'
-  const int blocks = (g.t * G + R - 1) / R, cost = kTreeStart + g.n;
-  const int u = x - __builtin_amdgcn_readfirstlane(s.cost[g.b]), grp = u / cost;
-  g.origin = x - (u - grp * cost) + kTreeStart;
-  g.c0 = max(x - g.origin, 0);
-  g.c1 = min(g.n, end - g.origin);
-  g.kvh = blocks == 1 ? grp : grp / blocks;
-  g.row0 = (grp - g.kvh * blocks) * R;
-  g.rows = min(R, g.t * G - g.row0);
+  const int rows = g.t * G, u = x - __builtin_amdgcn_readfirstlane(s.cost[deal][g.b]);
+  const int whole = group_cost<C>(R, g.n), all = groups_cost<C>(rows, g.n, R);
+  g.kvh = u / all;
+  const int in = u - g.kvh * all, grp = min(in / whole, (rows - 1) / R);
+  g.row0 = grp * R;
+  g.rows = min(R, rows - g.row0);
+  g.chunk = chunk_cost<C>(g.rows);
+  g.origin = x - (in - grp * whole) + kStart<C>;
+  // chunk i is the run's in which its cost begins
+  g.c0 = (max(x - g.origin, 0) + g.chunk - 1) / g.chunk;
+  g.c1 = min(g.n, (max(end - g.origin, 0) + g.chunk - 1) / g.chunk);
   return g;
 }
 
@@ -319,7 +352,7 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
   constexpr uint32_t kTile = kTreeChunk * D * 2, kRing = kStages<D> * 2 * kTile;
   static_assert(R * D * 4 <= kRing, "a wave's results fit its ring");
   __shared__ __attribute__((aligned(1024))) unsigned char lds[kTreeWaves * kRing];
-  __shared__ TreeBounds bounds;
+  __shared__ TreeBounds<1> bounds;
   __shared__ float ml[kTreeWaves][R][2];
   const PagedCache& c = a.c;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -331,8 +364,8 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
   const int w = __builtin_amdgcn_readfirstlane((blockIdx.x % kNumXcd) * per_xcd + blockIdx.x / kNumXcd);
 
   tree_bounds<R, kTreeChunk>(a, bounds);
-  const int total = __builtin_amdgcn_readfirstlane(bounds.cost[c.batch]);
-  const int run = max(kTreeMinRun, (total + kTreeGroups - 1) / kTreeGroups);
+  const int total = __builtin_amdgcn_readfirstlane(bounds.cost[0][c.batch]);
+  const int run = max(kMinRun<kTreeChunk>, (total + kTreeGroups - 1) / kTreeGroups);
   const int begin = int(min(int64_t(w) * run, int64_t(total))), end = int(min(int64_t(begin) + run, int64_t(total)));
   TreeSplit split{0, 0, 0, 0, 0};
 
@@ -346,9 +379,9 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
   for (int i = 0; i < kKinds; ++i) chunk16[i] = ((lane % CPR) ^ swz<D>(i * RPI + lrow)) * 8;
 
   for (int x = begin; x < end;) {
-    const TreeSegment seg = tree_segment<R, kTreeChunk>(a, bounds, G, x, end);
+    const TreeSegment seg = tree_segment<kTreeChunk>(a, bounds, 0, R, G, x, end);
     const int t0 = seg.t0, ctx = seg.ctx, n = seg.n, c0 = seg.c0, c1 = seg.c1;
-    x = seg.origin + n;
+    x = seg.behind();
     if (c0 >= c1) continue;  // the run ends before the group's first chunk
     const const_ints table = (const_ints)(uintptr_t)(c.table + int64_t(seg.b) * c.table_stride);
 
@@ -522,7 +555,7 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
       }
     }
     if (!whole && c0 == 0)  // the group's first keys
-      split = TreeSplit{(seg.origin + n - 1) / run - w + 1, t0, seg.row0, seg.rows, seg.kvh};
+      split = TreeSplit{seg.pieces(w, run), t0, seg.row0, seg.rows, seg.kvh};
     __syncthreads();  // the rings and ml are free again
   }
   if (threadIdx.x == 0) a.split[w] = split;
@@ -545,232 +578,254 @@ __device__ __forceinline__ void tree_half(FwdState<D, NQ>& st, const __bf16* kt,
   pv_half<D, NQ, SwizzledRows>(st, vt, pack_half<NQ>(s));
 }
 
+// Where the shared kernel's tiles lie.
+struct SharedTiles {
+  __bf16 *k[3], *v[3];
+};
+
+// The run's share of a group of at most 128 NQ rows, 16 NQ per wave; an unfinished group's results go to `part`.
+template <int D, int NQ>
+__device__ __forceinline__ void shared_group(const TreeArgs& a, const TreeSegment& seg, const SharedTiles& lds, float* part) {
+  constexpr int NC = D / 32, ND = D / 16, C = kSharedChunk;
+  using TL = SwzTile<D, C>;
+  constexpr int RPI = 512 / D, CPR = D / 8, kPer = TL::kInstr / kWaves;  // rows of a load instruction; a wave's of a tile
+  static_assert(kPer >= 1 && RPI * kWaves % 8 == 0 && C == kFwdKeyStep, "tiles by waves");
+  __bf16* const kb[3] = {lds.k[0], lds.k[1], lds.k[2]};
+  __bf16* const vb[3] = {lds.v[0], lds.v[1], lds.v[2]};
+  const PagedCache& c = a.c;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 4, l16 = lane & 15;
+  const int G = a.heads / c.kv_heads, page_mask = (1 << c.page_shift) - 1;
+  const float sl2 = a.scale_log2;
+  // load instructions wave + 8 j of a tile: rows RPI (wave + 8 j) + lane / CPR, one swizzle for all j
+  const int lrow = RPI * wave + lane / CPR, chunk16 = ((lane % CPR) ^ swz<D>(lrow)) * 8;
+  const uint32_t koff = (uint32_t((lane / CPR) * c.k_token) + chunk16) * 2;
+  const uint32_t voff = (uint32_t((lane / CPR) * c.v_token) + chunk16) * 2;
+  const int t0 = seg.t0, ctx = seg.ctx, n = seg.n, c0 = seg.c0, c1 = seg.c1;
+      const const_ints table = (const_ints)(uintptr_t)(c.table + int64_t(seg.b) * c.table_stride);
+      int T = max(0, min(c1, ctx / C) - c0);  // whole tiles of the context
+      bool bad = false;
+      if (T > 0)
+        for (int p = (c0 * C >> c.page_shift) + lane; p <= ((c0 + T) * C - 1) >> c.page_shift; p += 64)
+          bad |= uint32_t(c.table[int64_t(seg.b) * c.table_stride + p]) >= uint32_t(c.pages);
+      if (__builtin_amdgcn_ballot_w64(bad)) T = 0;
+
+      // page ids of this wave's load instructions of tile i (an instruction's rows lie in one 8-row part of a page)
+      struct Ids {
+        int v[kPer];
+      };
+      auto page_ids = [&](int i) __attribute__((always_inline)) {
+        Ids ids{};
+        if (i < c0 + T)
+  #pragma unroll
+          for (int j = 0; j < kPer; ++j) ids.v[j] = table[(i * C + RPI * (wave + j * kWaves)) >> c.page_shift];
+        return ids;
+      };
+      const uint64_t kbase = uniform_u64(reinterpret_cast<uint64_t>(c.k + int64_t(seg.kvh) * D));
+      const uint64_t vbase = uniform_u64(reinterpret_cast<uint64_t>(c.v + int64_t(seg.kvh) * D));
+      auto issue = [&](int i, const Ids& ids, bool is_v, const __bf16* dst) __attribute__((always_inline)) {
+        const uint32_t la = lds_addr(dst) + wave * 1024;
+  #pragma unroll
+        for (int j = 0; j < kPer; ++j) {
+          const int slot = (i * C + RPI * (wave + j * kWaves)) & page_mask;
+          lds_dma_x4_off(uniform_u64(page_row(is_v ? vbase : kbase, is_v ? a.v_step : a.k_step, ids.v[j], slot)),
+                         is_v ? voff : koff, la + j * kWaves * 1024);
+        }
+      };
+      int next_k = c0, next_v = c0;
+      Ids ids_k = page_ids(c0), ids_v = ids_k;  // of the tiles that are loaded next
+      auto issue_k = [&](const __bf16* dst) __attribute__((always_inline)) {
+        issue(next_k, ids_k, false, dst);
+        ids_k = page_ids(++next_k);
+      };
+      auto issue_v = [&](const __bf16* dst) __attribute__((always_inline)) {
+        issue(next_v, ids_v, true, dst);
+        ids_v = page_ids(++next_v);
+      };
+      if (T > 0) {
+        issue_k(kb[0]);
+        issue_v(vb[0]);
+        if (T > 1) issue_k(kb[1]);
+      }
+
+      FwdState<D, NQ> st;
+      const int wrow = wave * 16 * NQ;
+      const bool active = wrow < seg.rows;
+      const int tok0 = seg.row0 / G, rem0 = seg.row0 - tok0 * G;
+      auto row_of = [&](int qb) { return rem0 + min(wrow + 16 * qb + l16, seg.rows - 1); };
+  #pragma unroll
+      for (int qb = 0; qb < NQ; ++qb) {
+        const int r = row_of(qb), dt = group_div(a, G, r), h = seg.kvh * G + r - dt * G;
+        const __bf16* src = a.q + int64_t(t0 + tok0 + dt) * a.qs + int64_t(h) * D + g * 8;
+  #pragma unroll
+        for (int i = 0; i < NC; ++i) st.qf[qb][i] = ld8(src + i * 32);
+  #pragma unroll
+        for (int db = 0; db < ND; ++db) st.o[qb][db] = floatx4{};
+        st.m[qb] = -INFINITY;
+        st.l[qb] = 0.f;
+      }
+      // land them here, behind the first tiles, not at their first use inside the loop
+  #pragma unroll
+      for (int qb = 0; qb < NQ; ++qb)
+  #pragma unroll
+        for (int i = 0; i < NC; ++i) asm volatile("" : "+v"(st.qf[qb][i]));
+
+      // Tile t sits in K buffer t % 3 and V buffer t % 3 (tile -1 in V buffer 2). Iteration t reads K(t) (second half),
+      // K(t+1) (first half), V(t-1) (second half) and V(t) (first half), and loads K(t+2) and V(t+1).
+      if (T > 0) {
+        for (int e = threadIdx.x * 8; e < 32 * D; e += kWaves * 64 * 8)
+          *reinterpret_cast<bf16x8*>(vb[2] + 32 * D + e) = bf16x8{};
+        wait_vmem();
+        __syncthreads();
+        HalfP<NQ> p_hi;
+  #pragma unroll
+        for (int qb = 0; qb < NQ; ++qb) p_hi.p[qb] = bf16x8{};
+        HalfS<NQ> s_lo = {}, s_hi = {};
+        if (active) s_lo = scores32<D, NQ, SwizzledRows>(st, kb[0]);
+        Ahead ah;
+  #pragma unroll
+        for (int i = 0; i < kLook; ++i) {
+          ah.k[i] = k_frag<D, SwizzledRows>(kb[0] + 32 * D, i);
+          ah.v[i] = v_frag<D, SwizzledRows>(vb[2] + 32 * D, i);
+        }
+        auto iteration = [&](int t, auto phase) {
+          constexpr int P = decltype(phase)::value;
+          __bf16* const k_t = kb[P];
+          __bf16* const k_t1 = kb[(P + 1) % 3];
+          __bf16* const v_tm1 = vb[(P + 2) % 3];
+          __bf16* const v_t = vb[P];
+          if (t + 1 < T) issue_v(vb[(P + 1) % 3]);
+          if (t + 2 < T) issue_k(kb[(P + 2) % 3]);
+          if (active) {
+            const HalfP<NQ> p_lo = pipe_block<D, NQ, SwizzledRows>(st, s_lo, k_t, s_hi, k_t + 32 * D, v_tm1 + 32 * D, k_t1,
+                                                                   v_t, ah, p_hi, sl2);
+            p_hi = pipe_block<D, NQ, SwizzledRows>(st, s_hi, k_t + 32 * D, s_lo, k_t1, v_t, k_t1 + 32 * D, v_t + 32 * D, ah,
+                                                   p_lo, sl2);
+          }
+          wait_vmem();
+          __syncthreads();
+        };
+        using P0 = std::integral_constant<int, 0>;
+        using P1 = std::integral_constant<int, 1>;
+        using P2 = std::integral_constant<int, 2>;
+        int t = 0;
+        for (; t + 3 <= T; t += 3) {
+          iteration(t, P0{});
+          iteration(t + 1, P1{});
+          iteration(t + 2, P2{});
+        }
+        if (t < T) iteration(t, P0{});
+        if (t + 1 < T) iteration(t + 1, P1{});
+        if (active) {
+          const int last = (T - 1) % 3;
+          if (last == 0) pv_half<D, NQ, SwizzledRows>(st, vb[0] + 32 * D, p_hi);
+          else if (last == 1) pv_half<D, NQ, SwizzledRows>(st, vb[1] + 32 * D, p_hi);
+          else pv_half<D, NQ, SwizzledRows>(st, vb[2] + 32 * D, p_hi);
+        }
+      }
+
+      // the masked tiles
+      for (int i = c0 + T; i < c1; ++i) {
+        __syncthreads();  // every wave is done with the buffers
+        const TreeKey key = tree_key(a, seg, D, i * C + lane);
+        const uint64_t exist = __builtin_amdgcn_ballot_w64(key.exists);
+  #pragma unroll 1
+        for (int j = 0; j < kPer; ++j) {
+          const int r = lrow + j * RPI * kWaves;
+          lds_dma_x4_at(reinterpret_cast<const __bf16*>(lane_u64(key.k, r)) + chunk16, lds_addr(kb[0]) + (wave + j * kWaves) * 1024);
+          lds_dma_x4_at(reinterpret_cast<const __bf16*>(lane_u64(key.v, r)) + chunk16, lds_addr(vb[0]) + (wave + j * kWaves) * 1024);
+        }
+        uint64_t tree[NQ];  // which new tokens the lane's row sees
+        int tok[NQ];
+  #pragma unroll
+        for (int qb = 0; qb < NQ; ++qb) {
+          tok[qb] = tok0 + group_div(a, G, row_of(qb));
+          tree[qb] = a.tree ? a.tree[t0 + tok[qb]] : 0;
+        }
+        wait_vmem();
+        __syncthreads();
+        if (active)
+  #pragma unroll 1
+          for (int half = 0; half < 2; ++half) {
+            uint32_t vis[NQ];
+  #pragma unroll
+            for (int qb = 0; qb < NQ; ++qb)
+              vis[qb] = uint32_t(exist >> (32 * half)) & tree_word(a.tree, tree[qb], tok[qb], ctx - i * C - 32 * half);
+            tree_half<D, NQ>(st, kb[0] + half * 32 * D, vb[0] + half * 32 * D, vis, sl2);
+          }
+      }
+
+      const bool whole = c0 == 0 && c1 == n;
+          if (active) {
+  #pragma unroll
+        for (int qb = 0; qb < NQ; ++qb) {
+          const int r = wrow + 16 * qb + l16;
+          const float l = quad_sum(st.l[qb]);
+          if (r >= seg.rows) continue;
+          if (whole) {
+            const int rr = rem0 + r, dt = group_div(a, G, rr), h = seg.kvh * G + rr - dt * G;
+            const int64_t token = t0 + tok0 + dt;
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            __bf16* orow = a.o + (token * a.heads + h) * D + 4 * g;
+  #pragma unroll
+            for (int db = 0; db < ND; ++db) {
+              bf16x4 y;
+  #pragma unroll
+              for (int e = 0; e < 4; ++e) y[e] = (__bf16)(st.o[qb][db][e] * inv);
+              *reinterpret_cast<bf16x4*>(orow + db * 16) = y;
+            }
+            if (g == 0) a.lse[int64_t(h) * c.tokens + token] = l == 0.f ? -INFINITY : (st.m[qb] + log2f(l)) * kLn2;
+          } else {
+  #pragma unroll
+            for (int db = 0; db < ND; ++db) *reinterpret_cast<floatx4*>(part + r * D + db * 16 + 4 * g) = st.o[qb][db];
+            if (g == 0) *reinterpret_cast<float2*>(part + kTreeShared * D + 2 * r) = float2{st.m[qb], l};
+          }
+        }
+      }
+}
+
 // The same for many rows (trees of drafted tokens): up to 256 rows to a group, so that K and V are read once for all of
-// them. Eight waves (two per SIMD) own 32 rows each; the keys go through LDS in 64-key tiles that all of them read.
+// them, or 128 where that would split the groups of a short launch. Eight waves (two per SIMD) own 16 or 32 rows each, as
+// the group has up to 128 or more (32 for all of them: half of the waves idle, 6 % slower); the keys go through LDS in 64-key tiles that all of them read.
 // Whole tiles of the context run through the software pipeline of sra_fwd_pipe.h (three buffers each for K and V, loads
 // two and one tiles ahead), the context's end and the new tokens behind them, masked. Where the table names a page
 // that is none, all of the group's tiles run masked.
 template <int D>
 __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 sra_tree_shared_kernel(TreeArgs a) {
-  constexpr int NQ = 2, NC = D / 32, ND = D / 16, R = kTreeShared, C = kSharedChunk;
+  constexpr int C = kSharedChunk;
   using TL = SwzTile<D, C>;
-  constexpr int RPI = 512 / D, CPR = D / 8, kPer = TL::kInstr / kWaves;  // rows of a load instruction; a wave's of a tile
-  static_assert(R == kWaves * 16 * NQ && kPer >= 1 && RPI * kWaves % 8 == 0 && C == kFwdKeyStep, "tiles by waves");
   __shared__ __attribute__((aligned(1024))) __bf16 kbuf0[TL::kElems];
   __shared__ __attribute__((aligned(1024))) __bf16 kbuf1[TL::kElems];
   __shared__ __attribute__((aligned(1024))) __bf16 kbuf2[TL::kElems];
   __shared__ __attribute__((aligned(1024))) __bf16 vbuf0[TL::kElems];
   __shared__ __attribute__((aligned(1024))) __bf16 vbuf1[TL::kElems];
   __shared__ __attribute__((aligned(1024))) __bf16 vbuf2[TL::kElems];
-  __bf16* const kb[3] = {kbuf0, kbuf1, kbuf2};
-  __bf16* const vb[3] = {vbuf0, vbuf1, vbuf2};
-  __shared__ TreeBounds bounds;
+  const SharedTiles tiles{{kbuf0, kbuf1, kbuf2}, {vbuf0, vbuf1, vbuf2}};
+  __shared__ TreeBounds<2> bounds;
   const PagedCache& c = a.c;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int g = lane >> 4, l16 = lane & 15;
-  const int G = a.heads / c.kv_heads, page_mask = (1 << c.page_shift) - 1;
-  const float sl2 = a.scale_log2;
+  const int G = a.heads / c.kv_heads;
   constexpr int per_xcd = kTreeGroups / kNumXcd;
   const int w = __builtin_amdgcn_readfirstlane((blockIdx.x % kNumXcd) * per_xcd + blockIdx.x / kNumXcd);
 
-  tree_bounds<R, C>(a, bounds);
-  const int total = __builtin_amdgcn_readfirstlane(bounds.cost[c.batch]);
-  const int run = max(kTreeMinRun, (total + kTreeGroups - 1) / kTreeGroups);
+  tree_bounds<kTreeShared, C>(a, bounds);
+  int deal = 0, total = __builtin_amdgcn_readfirstlane(bounds.cost[0][c.batch]);
+  if (total < kSharedShortRun * kTreeGroups) {
+    deal = 1;
+    total = __builtin_amdgcn_readfirstlane(bounds.cost[1][c.batch]);
+  }
+  const int run = max(kMinRun<C>, (total + kTreeGroups - 1) / kTreeGroups);
   const int begin = int(min(int64_t(w) * run, int64_t(total))), end = int(min(int64_t(begin) + run, int64_t(total)));
   TreeSplit split{0, 0, 0, 0, 0};
-  // load instructions wave + 8 j of a tile: rows RPI (wave + 8 j) + lane / CPR, one swizzle for all j
-  const int lrow = RPI * wave + lane / CPR, chunk16 = ((lane % CPR) ^ swz<D>(lrow)) * 8;
-  const uint32_t koff = (uint32_t((lane / CPR) * c.k_token) + chunk16) * 2, voff = (uint32_t((lane / CPR) * c.v_token) + chunk16) * 2;
-
   for (int x = begin; x < end;) {
-    const TreeSegment seg = tree_segment<R, C>(a, bounds, G, x, end);
-    const int t0 = seg.t0, ctx = seg.ctx, n = seg.n, c0 = seg.c0, c1 = seg.c1;
-    x = seg.origin + n;
-    if (c0 >= c1) continue;  // the run ends before the group's first tile
-    const const_ints table = (const_ints)(uintptr_t)(c.table + int64_t(seg.b) * c.table_stride);
-    int T = max(0, min(c1, ctx / C) - c0);  // whole tiles of the context
-    bool bad = false;
-    if (T > 0)
-      for (int p = (c0 * C >> c.page_shift) + lane; p <= ((c0 + T) * C - 1) >> c.page_shift; p += 64)
-        bad |= uint32_t(c.table[int64_t(seg.b) * c.table_stride + p]) >= uint32_t(c.pages);
-    if (__builtin_amdgcn_ballot_w64(bad)) T = 0;
-
-    // page ids of this wave's load instructions of tile i (an instruction's rows lie in one 8-row part of a page)
-    struct Ids {
-      int v[kPer];
-    };
-    auto page_ids = [&](int i) __attribute__((always_inline)) {
-      Ids ids{};
-      if (i < c0 + T)
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) ids.v[j] = table[(i * C + RPI * (wave + j * kWaves)) >> c.page_shift];
-      return ids;
-    };
-    const uint64_t kbase = uniform_u64(reinterpret_cast<uint64_t>(c.k + int64_t(seg.kvh) * D));
-    const uint64_t vbase = uniform_u64(reinterpret_cast<uint64_t>(c.v + int64_t(seg.kvh) * D));
-    auto issue = [&](int i, const Ids& ids, bool is_v, const __bf16* dst) __attribute__((always_inline)) {
-      const uint32_t la = lds_addr(dst) + wave * 1024;
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) {
-        const int slot = (i * C + RPI * (wave + j * kWaves)) & page_mask;
-        lds_dma_x4_off(uniform_u64(page_row(is_v ? vbase : kbase, is_v ? a.v_step : a.k_step, ids.v[j], slot)),
-                       is_v ? voff : koff, la + j * kWaves * 1024);
-      }
-    };
-    int next_k = c0, next_v = c0;
-    Ids ids_k = page_ids(c0), ids_v = ids_k;  // of the tiles that are loaded next
-    auto issue_k = [&](const __bf16* dst) __attribute__((always_inline)) {
-      issue(next_k, ids_k, false, dst);
-      ids_k = page_ids(++next_k);
-    };
-    auto issue_v = [&](const __bf16* dst) __attribute__((always_inline)) {
-      issue(next_v, ids_v, true, dst);
-      ids_v = page_ids(++next_v);
-    };
-    if (T > 0) {
-      issue_k(kbuf0);
-      issue_v(vbuf0);
-      if (T > 1) issue_k(kbuf1);
-    }
-
-    FwdState<D, NQ> st;
-    const int wrow = wave * 16 * NQ;
-    const bool active = wrow < seg.rows;
-    const int tok0 = seg.row0 / G, rem0 = seg.row0 - tok0 * G;
-    auto row_of = [&](int qb) { return rem0 + min(wrow + 16 * qb + l16, seg.rows - 1); };
-#pragma unroll
-    for (int qb = 0; qb < NQ; ++qb) {
-      const int r = row_of(qb), dt = group_div(a, G, r), h = seg.kvh * G + r - dt * G;
-      const __bf16* src = a.q + int64_t(t0 + tok0 + dt) * a.qs + int64_t(h) * D + g * 8;
-#pragma unroll
-      for (int i = 0; i < NC; ++i) st.qf[qb][i] = ld8(src + i * 32);
-#pragma unroll
-      for (int db = 0; db < ND; ++db) st.o[qb][db] = floatx4{};
-      st.m[qb] = -INFINITY;
-      st.l[qb] = 0.f;
-    }
-    // land them here, behind the first tiles, not at their first use inside the loop
-#pragma unroll
-    for (int qb = 0; qb < NQ; ++qb)
-#pragma unroll
-      for (int i = 0; i < NC; ++i) asm volatile("" : "+v"(st.qf[qb][i]));
-
-    // Tile t sits in K buffer t % 3 and V buffer t % 3 (tile -1 in V buffer 2). Iteration t reads K(t) (second half),
-    // K(t+1) (first half), V(t-1) (second half) and V(t) (first half), and loads K(t+2) and V(t+1).
-    if (T > 0) {
-      for (int e = threadIdx.x * 8; e < 32 * D; e += kWaves * 64 * 8)
-        *reinterpret_cast<bf16x8*>(vbuf2 + 32 * D + e) = bf16x8{};
-      wait_vmem();
-      __syncthreads();
-      HalfP<NQ> p_hi;
-#pragma unroll
-      for (int qb = 0; qb < NQ; ++qb) p_hi.p[qb] = bf16x8{};
-      HalfS<NQ> s_lo = {}, s_hi = {};
-      if (active) s_lo = scores32<D, NQ, SwizzledRows>(st, kbuf0);
-      Ahead ah;
-#pragma unroll
-      for (int i = 0; i < kLook; ++i) {
-        ah.k[i] = k_frag<D, SwizzledRows>(kbuf0 + 32 * D, i);
-        ah.v[i] = v_frag<D, SwizzledRows>(vbuf2 + 32 * D, i);
-      }
-      auto iteration = [&](int t, auto phase) {
-        constexpr int P = decltype(phase)::value;
-        __bf16* const k_t = kb[P];
-        __bf16* const k_t1 = kb[(P + 1) % 3];
-        __bf16* const v_tm1 = vb[(P + 2) % 3];
-        __bf16* const v_t = vb[P];
-        if (t + 1 < T) issue_v(vb[(P + 1) % 3]);
-        if (t + 2 < T) issue_k(kb[(P + 2) % 3]);
-        if (active) {
-          const HalfP<NQ> p_lo = pipe_block<D, NQ, SwizzledRows>(st, s_lo, k_t, s_hi, k_t + 32 * D, v_tm1 + 32 * D, k_t1,
-                                                                 v_t, ah, p_hi, sl2);
-          p_hi = pipe_block<D, NQ, SwizzledRows>(st, s_hi, k_t + 32 * D, s_lo, k_t1, v_t, k_t1 + 32 * D, v_t + 32 * D, ah,
-                                                 p_lo, sl2);
-        }
-        wait_vmem();
-        __syncthreads();
-      };
-      using P0 = std::integral_constant<int, 0>;
-      using P1 = std::integral_constant<int, 1>;
-      using P2 = std::integral_constant<int, 2>;
-      int t = 0;
-      for (; t + 3 <= T; t += 3) {
-        iteration(t, P0{});
-        iteration(t + 1, P1{});
-        iteration(t + 2, P2{});
-      }
-      if (t < T) iteration(t, P0{});
-      if (t + 1 < T) iteration(t + 1, P1{});
-      if (active) {
-        const int last = (T - 1) % 3;
-        if (last == 0) pv_half<D, NQ, SwizzledRows>(st, vbuf0 + 32 * D, p_hi);
-        else if (last == 1) pv_half<D, NQ, SwizzledRows>(st, vbuf1 + 32 * D, p_hi);
-        else pv_half<D, NQ, SwizzledRows>(st, vbuf2 + 32 * D, p_hi);
-      }
-    }
-
-    // the masked tiles
-    for (int i = c0 + T; i < c1; ++i) {
-      __syncthreads();  // every wave is done with the buffers
-      const TreeKey key = tree_key(a, seg, D, i * C + lane);
-      const uint64_t exist = __builtin_amdgcn_ballot_w64(key.exists);
-#pragma unroll 1
-      for (int j = 0; j < kPer; ++j) {
-        const int r = lrow + j * RPI * kWaves;
-        lds_dma_x4_at(reinterpret_cast<const __bf16*>(lane_u64(key.k, r)) + chunk16, lds_addr(kbuf0) + (wave + j * kWaves) * 1024);
-        lds_dma_x4_at(reinterpret_cast<const __bf16*>(lane_u64(key.v, r)) + chunk16, lds_addr(vbuf0) + (wave + j * kWaves) * 1024);
-      }
-      uint64_t tree[NQ];  // which new tokens the lane's row sees
-      int tok[NQ];
-#pragma unroll
-      for (int qb = 0; qb < NQ; ++qb) {
-        tok[qb] = tok0 + group_div(a, G, row_of(qb));
-        tree[qb] = a.tree ? a.tree[t0 + tok[qb]] : 0;
-      }
-      wait_vmem();
-      __syncthreads();
-      if (active)
-#pragma unroll 1
-        for (int half = 0; half < 2; ++half) {
-          uint32_t vis[NQ];
-#pragma unroll
-          for (int qb = 0; qb < NQ; ++qb)
-            vis[qb] = uint32_t(exist >> (32 * half)) & tree_word(a.tree, tree[qb], tok[qb], ctx - i * C - 32 * half);
-          tree_half<D, NQ>(st, kbuf0 + half * 32 * D, vbuf0 + half * 32 * D, vis, sl2);
-        }
-    }
-
-    const bool whole = c0 == 0 && c1 == n;
-    float* const part = a.part + int64_t(2 * w + (c0 == 0)) * R * (D + 2);
-    if (active) {
-#pragma unroll
-      for (int qb = 0; qb < NQ; ++qb) {
-        const int r = wrow + 16 * qb + l16;
-        const float l = quad_sum(st.l[qb]);
-        if (r >= seg.rows) continue;
-        if (whole) {
-          const int rr = rem0 + r, dt = group_div(a, G, rr), h = seg.kvh * G + rr - dt * G;
-          const int64_t token = t0 + tok0 + dt;
-          const float inv = l == 0.f ? 0.f : 1.f / l;
-          __bf16* orow = a.o + (token * a.heads + h) * D + 4 * g;
-#pragma unroll
-          for (int db = 0; db < ND; ++db) {
-            bf16x4 y;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = (__bf16)(st.o[qb][db][e] * inv);
-            *reinterpret_cast<bf16x4*>(orow + db * 16) = y;
-          }
-          if (g == 0) a.lse[int64_t(h) * c.tokens + token] = l == 0.f ? -INFINITY : (st.m[qb] + log2f(l)) * kLn2;
-        } else {
-#pragma unroll
-          for (int db = 0; db < ND; ++db) *reinterpret_cast<floatx4*>(part + r * D + db * 16 + 4 * g) = st.o[qb][db];
-          if (g == 0) *reinterpret_cast<float2*>(part + R * D + 2 * r) = float2{st.m[qb], l};
-        }
-      }
-    }
-    if (!whole && c0 == 0)  // the group's first keys
-      split = TreeSplit{(seg.origin + n - 1) / run - w + 1, t0, seg.row0, seg.rows, seg.kvh};
+    const TreeSegment seg = tree_segment<C>(a, bounds, deal, kTreeShared >> deal, G, x, end);
+    x = seg.behind();
+    if (seg.c0 >= seg.c1) continue;  // the run ends before the group's first tile
+    float* const part = a.part + int64_t(2 * w + (seg.c0 == 0)) * kTreeShared * (D + 2);
+    if (seg.rows > kNarrow) shared_group<D, 2>(a, seg, tiles, part);
+    else shared_group<D, 1>(a, seg, tiles, part);
+    if (seg.c0 == 0 && seg.c1 < seg.n)  // the group's first keys
+      split = TreeSplit{seg.pieces(w, run), seg.t0, seg.row0, seg.rows, seg.kvh};
     __syncthreads();  // the buffers are free again
   }
   if (threadIdx.x == 0) a.split[w] = split;

@@ -343,3 +343,32 @@ def test_serving_loop_captured_and_eager():
             hist[b] = (hk, hv)
             for cache, want in ((kc, hk), (vc, hv)):
                 assert torch.equal(T.gather_cache(cache, table[b], want.shape[0]), want)
+
+
+@pytest.mark.parametrize("tree", [True, False])
+@pytest.mark.parametrize("heads,kv,d,page", [(80, 16, 128, 16), (64, 16, 64, 128)])
+def test_long_steps_with_groups_of_all_widths(heads, kv, d, page, tree):
+    """So much work for every workgroup that rows are taken 256 at a time: sequences with more than 128 rows for a K/V head
+    (and the rest of them), with fewer, with one token, without any. Then one of them with a page that is none."""
+    print("tree wide", heads, kv, d, tree, flush=True)
+    ctx, new = [4500, 63, 6001, 9000, 4032, 5, 7777, 20, 5000, 6400], [64, 48, 51, 30, 64, 60, 1, 0, 33, 26]
+    if not tree:
+        new[2] = 130
+    x, masks, cu = make(ctx, new, heads, kv, d, page, seed=30 + heads)
+    masks = masks if tree else None
+    o, lse = check(x, masks, ctx, cu)
+    k, v = (T.gather_cache(x[n], x["page_table"][4], 4032) for n in ("k_cache", "v_cache"))
+    x["page_table"][4, 2] = -1
+    bad_o, bad_lse = sra.tree_attention(**x, tree=masks)
+    a, b = cu[4], cu[5]
+    assert torch.equal(bad_o[:a], o[:a]) and torch.equal(bad_o[b:], o[b:])
+    assert torch.equal(bad_lse[:, :a], lse[:, :a]) and torch.equal(bad_lse[:, b:], lse[:, b:])
+    keep = [p for p in range(4032) if p // page != 2]
+    see = torch.ones(b - a, len(keep) + b - a, dtype=torch.bool, device="cuda").tril(len(keep))
+    if tree:
+        see[:, len(keep):] = (masks[a:b, None] >> torch.arange(b - a, device="cuda")) & 1 == 1
+    for h in (0, heads // 2, heads - 1):
+        g = h * kv // heads
+        kh, vh = (torch.cat([c[keep, g], x[n][a:b, g]]).double() for c, n in ((k, "k"), (v, "v")))
+        want, want_lse, _, eo, el = T.rows(x["q"][a:b, h].double(), kh, vh, see, 1 / math.sqrt(d))
+        assert T.within(bad_o[a:b, h], want, eo)[0] and T.within(bad_lse[h, a:b], want_lse, el)[0]
