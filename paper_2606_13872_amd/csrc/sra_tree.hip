@@ -786,7 +786,8 @@ __device__ __forceinline__ void shared_group(const TreeArgs& a, const TreeSegmen
 
 // The same for many rows (trees of drafted tokens): up to 256 rows to a group, so that K and V are read once for all of
 // them, or 128 where that would split the groups of a short launch. Eight waves (two per SIMD) own 16 or 32 rows each, as
-// the group has up to 128 or more (32 for all of them: half of the waves idle, 6 % slower); the keys go through LDS in 64-key tiles that all of them read.
+// the group has up to 128 or more (32 for all of them: half of the waves idle, 6 % slower); the keys go through LDS in
+// 64-key tiles that all of them read.
 // Whole tiles of the context run through the software pipeline of sra_fwd_pipe.h (three buffers each for K and V, loads
 // two and one tiles ahead), the context's end and the new tokens behind them, masked. Where the table names a page
 // that is none, all of the group's tiles run masked.
