@@ -15,25 +15,37 @@ namespace sra {
 
 namespace {
 
-// Costs in steps of a forward item (64 keys x 256 rows; 1.75 us at head_dim 128, measured, as the others are). A
-// dQ step computes three products to the forward's two, a dK/dV step four.
-constexpr double kStepCost[3] = {1.0, 1.5, 1.85};
-constexpr double kItemCost[3] = {2.9, 4.5, 6.0};  // an item's loads before the first product, diagonal and epilogue
-constexpr double kSlotCost[3] = {2.2, 2.2, 4.5};  // writing the 32-bit partial results of a piece
-constexpr double kCombineCost = 3.0;              // the combine launch,
-constexpr double kCombineSlot = 0.025;            // and reading a piece's results there
-// A step of a large forward item (384 or 512 rows) to one of 256 rows: 0.93 times the work's share.
+// Costs of a kind of items, in steps of its launch's unit.
+struct Cost {
+  double step;            // 64 keys (dK/dV: 64 tokens)
+  double item;            // its loads before the first product, diagonal and epilogue
+  double slot;            // writing the 32-bit partial results of a piece
+  double combine, part;   // the combine launch, and reading a piece's results there
+};
+// Forward, in steps of 256 rows (1.4 us at head_dim 128, 1.05 at 64 where power does not bound them). Fitted to 44
+// sets of lengths, each with the items of 128 and of 256 rows cut at six lengths: what is chosen by them is 1.6 % slower
+// than the best of the twelve on average, 15 % at most (items of 256 rows alone: 20 and 70 %).
+constexpr Cost kSmallForward = {0.62, 4.2, 0.2, 2.75, 0.009};  // 128 rows
+constexpr Cost kForwardCost = {1.0, 5.9, 1.7, 2.75, 0.009};    // 256 rows
+// A step of a large item (384 or 512 rows) to one of 256 rows: 0.93 times the work's share.
 constexpr double large_step(int head_dim) { return 0.93 * fwd_large_tile(head_dim) / kCausalTile; }
-// Steps of 64 head dims take 0.6 times as long, what does not depend on them is worth more of them.
-constexpr double fixed_cost(int head_dim) { return head_dim == 128 ? 1.0 : 1.7; }
+constexpr int kSmallTile = kCausalTile / 2;
+// Backward, in forward steps of a launch that power bounds (1.75 us): a dQ step computes three products to the
+// forward's two, a dK/dV step four. Steps of 64 head dims take 0.6 times as long, what does not depend on them is
+// worth more of them.
+constexpr double kFixed64 = 1.7;
+constexpr Cost backward_cost(CausalKind kind, int head_dim) {
+  const double f = head_dim == 128 ? 1.0 : kFixed64;
+  return kind == kDq ? Cost{1.5, 4.5 * f, 2.2 * f, 3.0 * f, 0.025} : Cost{1.85, 6.0 * f, 4.5 * f, 3.0 * f, 0.05};
+}
 constexpr int kMaxSplit = 32;
 constexpr size_t kSplitItems = 2048;   // launches of more items are not cut (eight rounds of 256)
 
 struct Unit {
   CausalItem it;
   int32_t steps;
-  double step;  // cost of one
-  double cost() const { return steps * step; }
+  const Cost* each;
+  double cost() const { return steps * each->step; }
 };
 
 int pieces_of(const Unit& u, double cap) {
@@ -43,16 +55,19 @@ int pieces_of(const Unit& u, double cap) {
 }
 
 // When the last of the launch's pieces ends, launched longest first on 256 compute units.
-double replay(const std::vector<Unit>& units, double cap, double fixed) {
+double replay(const std::vector<Unit>& units, double cap) {
   std::vector<double> c;
   c.reserve(units.size() * 2);
-  double combine = 0;
+  double combine = 0, parts = 0;
   for (const Unit& u : units) {
     const int n = pieces_of(u, cap);
-    if (n > 1) combine += n * kCombineSlot * (u.it.kind == kDkv ? 2 : 1);
+    if (n > 1) {
+      combine = u.each->combine;
+      parts += n * u.each->part;
+    }
     for (int i = 0; i < n; ++i) {
       const int steps = u.steps * (i + 1) / n - u.steps * i / n;
-      c.push_back(fixed * kItemCost[u.it.kind] + steps * u.step + (n > 1 ? kSlotCost[u.it.kind] : 0.0));
+      c.push_back(u.each->item + steps * u.each->step + (n > 1 ? u.each->slot : 0.0));
     }
   }
   std::sort(c.begin(), c.end(), std::greater<double>());
@@ -69,17 +84,17 @@ double replay(const std::vector<Unit>& units, double cap, double fixed) {
     heap[i] = t;
     end = std::max(end, t);
   }
-  return end + (combine > 0 ? fixed * kCombineCost + combine : 0.0);
+  return end + combine + parts;
 }
 
 // The cost from which on items are cut (0: none is), and when the launch then ends.
-double choose_cap(const std::vector<Unit>& units, double fixed, double* end) {
+double choose_cap(const std::vector<Unit>& units, double* end) {
   double total = 0;
   for (const Unit& u : units) total += u.cost();
-  double best_cap = 0, best = replay(units, 0, fixed);
+  double best_cap = 0, best = replay(units, 0);
   for (double f : {2.0, 1.5, 1.2, 1.1, 1.0, 0.8, 0.65, 0.5, 0.35}) {
     const double cap = std::max(f * total / kNumCus, 4.0);
-    const double t = replay(units, cap, fixed);
+    const double t = replay(units, cap);
     if (t < 0.97 * best) best = t, best_cap = cap;
   }
   if (end) *end = best;
@@ -109,7 +124,7 @@ void emit(const std::vector<Unit>& units, double cap, std::vector<CausalItem>* i
         x.hi = std::min(64 * b, u.it.hi);
       }
       if (n > 1) x.slot = ++slots[u.it.kind];
-      out.emplace_back((b - a) * u.step, x);
+      out.emplace_back((b - a) * u.each->step, x);
     }
   }
   std::stable_sort(out.begin(), out.end(), [](const auto& a, const auto& b) { return a.first > b.first; });
@@ -120,9 +135,8 @@ void emit(const std::vector<Unit>& units, double cap, std::vector<CausalItem>* i
 
 void build_causal_tables(CausalTables* t) {
   const int32_t G = t->heads / t->kv_heads;
-  const double fixed = fixed_cost(t->head_dim);
   // Items of `tile` rows or keys each, K/V heads innermost.
-  auto units = [&](CausalKind kind, int32_t tile, double step) {
+  auto units = [&](CausalKind kind, int32_t tile, const Cost& each) {
     std::vector<Unit> out;
     int32_t q0 = 0, k0 = 0;
     for (int32_t b = 0; b < t->batch; ++b) {
@@ -137,7 +151,7 @@ void build_causal_tables(CausalTables* t) {
           it.hi = std::max(0, (r + it.len - 1) / G + nk - nq + 1);  // keys seen by the last row
           steps = (it.hi + 63) / 64;
         }
-        for (it.kvh = 0; it.kvh < t->kv_heads; ++it.kvh) out.push_back({it, steps, step});
+        for (it.kvh = 0; it.kvh < t->kv_heads; ++it.kvh) out.push_back({it, steps, &each});
       }
       q0 += nq;
       k0 += nk;
@@ -145,23 +159,33 @@ void build_causal_tables(CausalTables* t) {
     return out;
   };
   int32_t slots[3] = {0, 0, 0};
-  std::vector<Unit> fwd = units(kForward, kCausalTile, kStepCost[kForward]);
-  double cap = 0, end = 0;
-  t->fwd_tile = fwd_large_tile(t->head_dim);
-  if (fwd.size() <= kSplitItems) {  // larger items, or these, cut or not: whichever end first
-    cap = choose_cap(fwd, fixed, &end);
-    if (end <= replay(units(kForward, t->fwd_tile, large_step(t->head_dim)), 0, fixed)) t->fwd_tile = kCausalTile;
-  }
-  if (t->fwd_tile != kCausalTile) {
-    fwd = units(kForward, t->fwd_tile, large_step(t->head_dim));
-    cap = 0;
+  Cost large = kForwardCost;
+  large.step = large_step(t->head_dim);
+  std::vector<Unit> fwd = units(kForward, t->fwd_tile = fwd_large_tile(t->head_dim), large);
+  double cap = 0;
+  // larger items, or items of 256 or 128 rows, cut or not: whichever end first
+  std::vector<Unit> less = units(kForward, kCausalTile, kForwardCost);
+  if (less.size() <= kSplitItems) {
+    double end = replay(fwd, 0);
+    auto consider = [&](std::vector<Unit>&& u, int32_t tile) {
+      double at;
+      const double c = choose_cap(u, &at);
+      if (at > end) return;
+      end = at;
+      cap = c;
+      fwd = std::move(u);
+      t->fwd_tile = tile;
+    };
+    consider(std::move(less), kCausalTile);
+    consider(units(kForward, kSmallTile, kSmallForward), kSmallTile);
   }
   emit(fwd, cap, &t->fwd, &t->fwd_combine, slots);
   if (t->backward) {
-    std::vector<Unit> dkv = units(kDkv, kCausalTile, kStepCost[kDkv]), dq = units(kDq, kCausalTile, kStepCost[kDq]);
+    const Cost dkv_cost = backward_cost(kDkv, t->head_dim), dq_cost = backward_cost(kDq, t->head_dim);
+    std::vector<Unit> dkv = units(kDkv, kCausalTile, dkv_cost), dq = units(kDq, kCausalTile, dq_cost);
     if (dq.size() + dkv.size() <= kSplitItems) {  // few items: both kinds together, each fills the other's gaps
       dkv.insert(dkv.end(), dq.begin(), dq.end());
-      emit(dkv, choose_cap(dkv, fixed, nullptr), &t->grad, &t->grad_combine, slots);
+      emit(dkv, choose_cap(dkv, nullptr), &t->grad, &t->grad_combine, slots);
     } else {  // many: one kind after the other, so that an XCD streams one kind of rows at a time
       emit(dkv, 0, &t->grad, &t->grad_combine, slots);
       emit(dq, 0, &t->grad, &t->grad_combine, slots);

@@ -269,10 +269,12 @@ hipError_t launch_causal_forward(const CausalArgs& a, int n_items, int head_dim,
   if (n_items <= 0) return hipSuccess;
   constexpr int kRows = 16 * kWaves;
   if (head_dim == 128) {
-    if (tile == kCausalTile) launch_tile<128, kCausalTile / kRows>(a, n_items, stream);
+    if (tile < kCausalTile) launch_tile<128, 1>(a, n_items, stream);
+    else if (tile == kCausalTile) launch_tile<128, kCausalTile / kRows>(a, n_items, stream);
     else launch_tile<128, fwd_large_tile(128) / kRows>(a, n_items, stream);
   } else {
-    if (tile == kCausalTile) launch_tile<64, kCausalTile / kRows>(a, n_items, stream);
+    if (tile < kCausalTile) launch_tile<64, 1>(a, n_items, stream);
+    else if (tile == kCausalTile) launch_tile<64, kCausalTile / kRows>(a, n_items, stream);
     else launch_tile<64, fwd_large_tile(64) / kRows>(a, n_items, stream);
   }
   return hipGetLastError();
