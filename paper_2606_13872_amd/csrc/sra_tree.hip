@@ -602,186 +602,186 @@ __device__ __forceinline__ void shared_group(const TreeArgs& a, const TreeSegmen
   const uint32_t koff = (uint32_t((lane / CPR) * c.k_token) + chunk16) * 2;
   const uint32_t voff = (uint32_t((lane / CPR) * c.v_token) + chunk16) * 2;
   const int t0 = seg.t0, ctx = seg.ctx, n = seg.n, c0 = seg.c0, c1 = seg.c1;
-      const const_ints table = (const_ints)(uintptr_t)(c.table + int64_t(seg.b) * c.table_stride);
-      int T = max(0, min(c1, ctx / C) - c0);  // whole tiles of the context
-      bool bad = false;
-      if (T > 0)
-        for (int p = (c0 * C >> c.page_shift) + lane; p <= ((c0 + T) * C - 1) >> c.page_shift; p += 64)
-          bad |= uint32_t(c.table[int64_t(seg.b) * c.table_stride + p]) >= uint32_t(c.pages);
-      if (__builtin_amdgcn_ballot_w64(bad)) T = 0;
+  const const_ints table = (const_ints)(uintptr_t)(c.table + int64_t(seg.b) * c.table_stride);
+  int T = max(0, min(c1, ctx / C) - c0);  // whole tiles of the context
+  bool bad = false;
+  if (T > 0)
+    for (int p = (c0 * C >> c.page_shift) + lane; p <= ((c0 + T) * C - 1) >> c.page_shift; p += 64)
+      bad |= uint32_t(c.table[int64_t(seg.b) * c.table_stride + p]) >= uint32_t(c.pages);
+  if (__builtin_amdgcn_ballot_w64(bad)) T = 0;
 
-      // page ids of this wave's load instructions of tile i (an instruction's rows lie in one 8-row part of a page)
-      struct Ids {
-        int v[kPer];
-      };
-      auto page_ids = [&](int i) __attribute__((always_inline)) {
-        Ids ids{};
-        if (i < c0 + T)
-  #pragma unroll
-          for (int j = 0; j < kPer; ++j) ids.v[j] = table[(i * C + RPI * (wave + j * kWaves)) >> c.page_shift];
-        return ids;
-      };
-      const uint64_t kbase = uniform_u64(reinterpret_cast<uint64_t>(c.k + int64_t(seg.kvh) * D));
-      const uint64_t vbase = uniform_u64(reinterpret_cast<uint64_t>(c.v + int64_t(seg.kvh) * D));
-      auto issue = [&](int i, const Ids& ids, bool is_v, const __bf16* dst) __attribute__((always_inline)) {
-        const uint32_t la = lds_addr(dst) + wave * 1024;
-  #pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-          const int slot = (i * C + RPI * (wave + j * kWaves)) & page_mask;
-          lds_dma_x4_off(uniform_u64(page_row(is_v ? vbase : kbase, is_v ? a.v_step : a.k_step, ids.v[j], slot)),
-                         is_v ? voff : koff, la + j * kWaves * 1024);
-        }
-      };
-      int next_k = c0, next_v = c0;
-      Ids ids_k = page_ids(c0), ids_v = ids_k;  // of the tiles that are loaded next
-      auto issue_k = [&](const __bf16* dst) __attribute__((always_inline)) {
-        issue(next_k, ids_k, false, dst);
-        ids_k = page_ids(++next_k);
-      };
-      auto issue_v = [&](const __bf16* dst) __attribute__((always_inline)) {
-        issue(next_v, ids_v, true, dst);
-        ids_v = page_ids(++next_v);
-      };
-      if (T > 0) {
-        issue_k(kb[0]);
-        issue_v(vb[0]);
-        if (T > 1) issue_k(kb[1]);
-      }
+  // page ids of this wave's load instructions of tile i (an instruction's rows lie in one 8-row part of a page)
+  struct Ids {
+    int v[kPer];
+  };
+  auto page_ids = [&](int i) __attribute__((always_inline)) {
+    Ids ids{};
+    if (i < c0 + T)
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) ids.v[j] = table[(i * C + RPI * (wave + j * kWaves)) >> c.page_shift];
+    return ids;
+  };
+  const uint64_t kbase = uniform_u64(reinterpret_cast<uint64_t>(c.k + int64_t(seg.kvh) * D));
+  const uint64_t vbase = uniform_u64(reinterpret_cast<uint64_t>(c.v + int64_t(seg.kvh) * D));
+  auto issue = [&](int i, const Ids& ids, bool is_v, const __bf16* dst) __attribute__((always_inline)) {
+    const uint32_t la = lds_addr(dst) + wave * 1024;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int slot = (i * C + RPI * (wave + j * kWaves)) & page_mask;
+      lds_dma_x4_off(uniform_u64(page_row(is_v ? vbase : kbase, is_v ? a.v_step : a.k_step, ids.v[j], slot)),
+                     is_v ? voff : koff, la + j * kWaves * 1024);
+    }
+  };
+  int next_k = c0, next_v = c0;
+  Ids ids_k = page_ids(c0), ids_v = ids_k;  // of the tiles that are loaded next
+  auto issue_k = [&](const __bf16* dst) __attribute__((always_inline)) {
+    issue(next_k, ids_k, false, dst);
+    ids_k = page_ids(++next_k);
+  };
+  auto issue_v = [&](const __bf16* dst) __attribute__((always_inline)) {
+    issue(next_v, ids_v, true, dst);
+    ids_v = page_ids(++next_v);
+  };
+  if (T > 0) {
+    issue_k(kb[0]);
+    issue_v(vb[0]);
+    if (T > 1) issue_k(kb[1]);
+  }
 
-      FwdState<D, NQ> st;
-      const int wrow = wave * 16 * NQ;
-      const bool active = wrow < seg.rows;
-      const int tok0 = seg.row0 / G, rem0 = seg.row0 - tok0 * G;
-      auto row_of = [&](int qb) { return rem0 + min(wrow + 16 * qb + l16, seg.rows - 1); };
-  #pragma unroll
-      for (int qb = 0; qb < NQ; ++qb) {
-        const int r = row_of(qb), dt = group_div(a, G, r), h = seg.kvh * G + r - dt * G;
-        const __bf16* src = a.q + int64_t(t0 + tok0 + dt) * a.qs + int64_t(h) * D + g * 8;
-  #pragma unroll
-        for (int i = 0; i < NC; ++i) st.qf[qb][i] = ld8(src + i * 32);
-  #pragma unroll
-        for (int db = 0; db < ND; ++db) st.o[qb][db] = floatx4{};
-        st.m[qb] = -INFINITY;
-        st.l[qb] = 0.f;
-      }
-      // land them here, behind the first tiles, not at their first use inside the loop
-  #pragma unroll
-      for (int qb = 0; qb < NQ; ++qb)
-  #pragma unroll
-        for (int i = 0; i < NC; ++i) asm volatile("" : "+v"(st.qf[qb][i]));
+  FwdState<D, NQ> st;
+  const int wrow = wave * 16 * NQ;
+  const bool active = wrow < seg.rows;
+  const int tok0 = seg.row0 / G, rem0 = seg.row0 - tok0 * G;
+  auto row_of = [&](int qb) { return rem0 + min(wrow + 16 * qb + l16, seg.rows - 1); };
+#pragma unroll
+  for (int qb = 0; qb < NQ; ++qb) {
+    const int r = row_of(qb), dt = group_div(a, G, r), h = seg.kvh * G + r - dt * G;
+    const __bf16* src = a.q + int64_t(t0 + tok0 + dt) * a.qs + int64_t(h) * D + g * 8;
+#pragma unroll
+    for (int i = 0; i < NC; ++i) st.qf[qb][i] = ld8(src + i * 32);
+#pragma unroll
+    for (int db = 0; db < ND; ++db) st.o[qb][db] = floatx4{};
+    st.m[qb] = -INFINITY;
+    st.l[qb] = 0.f;
+  }
+  // land them here, behind the first tiles, not at their first use inside the loop
+#pragma unroll
+  for (int qb = 0; qb < NQ; ++qb)
+#pragma unroll
+    for (int i = 0; i < NC; ++i) asm volatile("" : "+v"(st.qf[qb][i]));
 
-      // Tile t sits in K buffer t % 3 and V buffer t % 3 (tile -1 in V buffer 2). Iteration t reads K(t) (second half),
-      // K(t+1) (first half), V(t-1) (second half) and V(t) (first half), and loads K(t+2) and V(t+1).
-      if (T > 0) {
-        for (int e = threadIdx.x * 8; e < 32 * D; e += kWaves * 64 * 8)
-          *reinterpret_cast<bf16x8*>(vb[2] + 32 * D + e) = bf16x8{};
-        wait_vmem();
-        __syncthreads();
-        HalfP<NQ> p_hi;
-  #pragma unroll
-        for (int qb = 0; qb < NQ; ++qb) p_hi.p[qb] = bf16x8{};
-        HalfS<NQ> s_lo = {}, s_hi = {};
-        if (active) s_lo = scores32<D, NQ, SwizzledRows>(st, kb[0]);
-        Ahead ah;
-  #pragma unroll
-        for (int i = 0; i < kLook; ++i) {
-          ah.k[i] = k_frag<D, SwizzledRows>(kb[0] + 32 * D, i);
-          ah.v[i] = v_frag<D, SwizzledRows>(vb[2] + 32 * D, i);
-        }
-        auto iteration = [&](int t, auto phase) {
-          constexpr int P = decltype(phase)::value;
-          __bf16* const k_t = kb[P];
-          __bf16* const k_t1 = kb[(P + 1) % 3];
-          __bf16* const v_tm1 = vb[(P + 2) % 3];
-          __bf16* const v_t = vb[P];
-          if (t + 1 < T) issue_v(vb[(P + 1) % 3]);
-          if (t + 2 < T) issue_k(kb[(P + 2) % 3]);
-          if (active) {
-            const HalfP<NQ> p_lo = pipe_block<D, NQ, SwizzledRows>(st, s_lo, k_t, s_hi, k_t + 32 * D, v_tm1 + 32 * D, k_t1,
-                                                                   v_t, ah, p_hi, sl2);
-            p_hi = pipe_block<D, NQ, SwizzledRows>(st, s_hi, k_t + 32 * D, s_lo, k_t1, v_t, k_t1 + 32 * D, v_t + 32 * D, ah,
-                                                   p_lo, sl2);
-          }
-          wait_vmem();
-          __syncthreads();
-        };
-        using P0 = std::integral_constant<int, 0>;
-        using P1 = std::integral_constant<int, 1>;
-        using P2 = std::integral_constant<int, 2>;
-        int t = 0;
-        for (; t + 3 <= T; t += 3) {
-          iteration(t, P0{});
-          iteration(t + 1, P1{});
-          iteration(t + 2, P2{});
-        }
-        if (t < T) iteration(t, P0{});
-        if (t + 1 < T) iteration(t + 1, P1{});
-        if (active) {
-          const int last = (T - 1) % 3;
-          if (last == 0) pv_half<D, NQ, SwizzledRows>(st, vb[0] + 32 * D, p_hi);
-          else if (last == 1) pv_half<D, NQ, SwizzledRows>(st, vb[1] + 32 * D, p_hi);
-          else pv_half<D, NQ, SwizzledRows>(st, vb[2] + 32 * D, p_hi);
-        }
+  // Tile t sits in K buffer t % 3 and V buffer t % 3 (tile -1 in V buffer 2). Iteration t reads K(t) (second half),
+  // K(t+1) (first half), V(t-1) (second half) and V(t) (first half), and loads K(t+2) and V(t+1).
+  if (T > 0) {
+    for (int e = threadIdx.x * 8; e < 32 * D; e += kWaves * 64 * 8)
+      *reinterpret_cast<bf16x8*>(vb[2] + 32 * D + e) = bf16x8{};
+    wait_vmem();
+    __syncthreads();
+    HalfP<NQ> p_hi;
+#pragma unroll
+    for (int qb = 0; qb < NQ; ++qb) p_hi.p[qb] = bf16x8{};
+    HalfS<NQ> s_lo = {}, s_hi = {};
+    if (active) s_lo = scores32<D, NQ, SwizzledRows>(st, kb[0]);
+    Ahead ah;
+#pragma unroll
+    for (int i = 0; i < kLook; ++i) {
+      ah.k[i] = k_frag<D, SwizzledRows>(kb[0] + 32 * D, i);
+      ah.v[i] = v_frag<D, SwizzledRows>(vb[2] + 32 * D, i);
+    }
+    auto iteration = [&](int t, auto phase) {
+      constexpr int P = decltype(phase)::value;
+      __bf16* const k_t = kb[P];
+      __bf16* const k_t1 = kb[(P + 1) % 3];
+      __bf16* const v_tm1 = vb[(P + 2) % 3];
+      __bf16* const v_t = vb[P];
+      if (t + 1 < T) issue_v(vb[(P + 1) % 3]);
+      if (t + 2 < T) issue_k(kb[(P + 2) % 3]);
+      if (active) {
+        const HalfP<NQ> p_lo = pipe_block<D, NQ, SwizzledRows>(st, s_lo, k_t, s_hi, k_t + 32 * D, v_tm1 + 32 * D, k_t1,
+                                                               v_t, ah, p_hi, sl2);
+        p_hi = pipe_block<D, NQ, SwizzledRows>(st, s_hi, k_t + 32 * D, s_lo, k_t1, v_t, k_t1 + 32 * D, v_t + 32 * D, ah,
+                                               p_lo, sl2);
       }
+      wait_vmem();
+      __syncthreads();
+    };
+    using P0 = std::integral_constant<int, 0>;
+    using P1 = std::integral_constant<int, 1>;
+    using P2 = std::integral_constant<int, 2>;
+    int t = 0;
+    for (; t + 3 <= T; t += 3) {
+      iteration(t, P0{});
+      iteration(t + 1, P1{});
+      iteration(t + 2, P2{});
+    }
+    if (t < T) iteration(t, P0{});
+    if (t + 1 < T) iteration(t + 1, P1{});
+    if (active) {
+      const int last = (T - 1) % 3;
+      if (last == 0) pv_half<D, NQ, SwizzledRows>(st, vb[0] + 32 * D, p_hi);
+      else if (last == 1) pv_half<D, NQ, SwizzledRows>(st, vb[1] + 32 * D, p_hi);
+      else pv_half<D, NQ, SwizzledRows>(st, vb[2] + 32 * D, p_hi);
+    }
+  }
 
-      // the masked tiles
-      for (int i = c0 + T; i < c1; ++i) {
-        __syncthreads();  // every wave is done with the buffers
-        const TreeKey key = tree_key(a, seg, D, i * C + lane);
-        const uint64_t exist = __builtin_amdgcn_ballot_w64(key.exists);
-  #pragma unroll 1
-        for (int j = 0; j < kPer; ++j) {
-          const int r = lrow + j * RPI * kWaves;
-          lds_dma_x4_at(reinterpret_cast<const __bf16*>(lane_u64(key.k, r)) + chunk16, lds_addr(kb[0]) + (wave + j * kWaves) * 1024);
-          lds_dma_x4_at(reinterpret_cast<const __bf16*>(lane_u64(key.v, r)) + chunk16, lds_addr(vb[0]) + (wave + j * kWaves) * 1024);
-        }
-        uint64_t tree[NQ];  // which new tokens the lane's row sees
-        int tok[NQ];
-  #pragma unroll
-        for (int qb = 0; qb < NQ; ++qb) {
-          tok[qb] = tok0 + group_div(a, G, row_of(qb));
-          tree[qb] = a.tree ? a.tree[t0 + tok[qb]] : 0;
-        }
-        wait_vmem();
-        __syncthreads();
-        if (active)
-  #pragma unroll 1
-          for (int half = 0; half < 2; ++half) {
-            uint32_t vis[NQ];
-  #pragma unroll
-            for (int qb = 0; qb < NQ; ++qb)
-              vis[qb] = uint32_t(exist >> (32 * half)) & tree_word(a.tree, tree[qb], tok[qb], ctx - i * C - 32 * half);
-            tree_half<D, NQ>(st, kb[0] + half * 32 * D, vb[0] + half * 32 * D, vis, sl2);
-          }
+  // the masked tiles
+  for (int i = c0 + T; i < c1; ++i) {
+    __syncthreads();  // every wave is done with the buffers
+    const TreeKey key = tree_key(a, seg, D, i * C + lane);
+    const uint64_t exist = __builtin_amdgcn_ballot_w64(key.exists);
+#pragma unroll 1
+    for (int j = 0; j < kPer; ++j) {
+      const int r = lrow + j * RPI * kWaves;
+      lds_dma_x4_at(reinterpret_cast<const __bf16*>(lane_u64(key.k, r)) + chunk16, lds_addr(kb[0]) + (wave + j * kWaves) * 1024);
+      lds_dma_x4_at(reinterpret_cast<const __bf16*>(lane_u64(key.v, r)) + chunk16, lds_addr(vb[0]) + (wave + j * kWaves) * 1024);
+    }
+    uint64_t tree[NQ];  // which new tokens the lane's row sees
+    int tok[NQ];
+#pragma unroll
+    for (int qb = 0; qb < NQ; ++qb) {
+      tok[qb] = tok0 + group_div(a, G, row_of(qb));
+      tree[qb] = a.tree ? a.tree[t0 + tok[qb]] : 0;
+    }
+    wait_vmem();
+    __syncthreads();
+    if (active)
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half) {
+        uint32_t vis[NQ];
+#pragma unroll
+        for (int qb = 0; qb < NQ; ++qb)
+          vis[qb] = uint32_t(exist >> (32 * half)) & tree_word(a.tree, tree[qb], tok[qb], ctx - i * C - 32 * half);
+        tree_half<D, NQ>(st, kb[0] + half * 32 * D, vb[0] + half * 32 * D, vis, sl2);
       }
+  }
 
-      const bool whole = c0 == 0 && c1 == n;
-          if (active) {
-  #pragma unroll
-        for (int qb = 0; qb < NQ; ++qb) {
-          const int r = wrow + 16 * qb + l16;
-          const float l = quad_sum(st.l[qb]);
-          if (r >= seg.rows) continue;
-          if (whole) {
-            const int rr = rem0 + r, dt = group_div(a, G, rr), h = seg.kvh * G + rr - dt * G;
-            const int64_t token = t0 + tok0 + dt;
-            const float inv = l == 0.f ? 0.f : 1.f / l;
-            __bf16* orow = a.o + (token * a.heads + h) * D + 4 * g;
-  #pragma unroll
-            for (int db = 0; db < ND; ++db) {
-              bf16x4 y;
-  #pragma unroll
-              for (int e = 0; e < 4; ++e) y[e] = (__bf16)(st.o[qb][db][e] * inv);
-              *reinterpret_cast<bf16x4*>(orow + db * 16) = y;
-            }
-            if (g == 0) a.lse[int64_t(h) * c.tokens + token] = l == 0.f ? -INFINITY : (st.m[qb] + log2f(l)) * kLn2;
-          } else {
-  #pragma unroll
-            for (int db = 0; db < ND; ++db) *reinterpret_cast<floatx4*>(part + r * D + db * 16 + 4 * g) = st.o[qb][db];
-            if (g == 0) *reinterpret_cast<float2*>(part + kTreeShared * D + 2 * r) = float2{st.m[qb], l};
-          }
+  const bool whole = c0 == 0 && c1 == n;
+      if (active) {
+#pragma unroll
+    for (int qb = 0; qb < NQ; ++qb) {
+      const int r = wrow + 16 * qb + l16;
+      const float l = quad_sum(st.l[qb]);
+      if (r >= seg.rows) continue;
+      if (whole) {
+        const int rr = rem0 + r, dt = group_div(a, G, rr), h = seg.kvh * G + rr - dt * G;
+        const int64_t token = t0 + tok0 + dt;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        __bf16* orow = a.o + (token * a.heads + h) * D + 4 * g;
+#pragma unroll
+        for (int db = 0; db < ND; ++db) {
+          bf16x4 y;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = (__bf16)(st.o[qb][db][e] * inv);
+          *reinterpret_cast<bf16x4*>(orow + db * 16) = y;
         }
+        if (g == 0) a.lse[int64_t(h) * c.tokens + token] = l == 0.f ? -INFINITY : (st.m[qb] + log2f(l)) * kLn2;
+      } else {
+#pragma unroll
+        for (int db = 0; db < ND; ++db) *reinterpret_cast<floatx4*>(part + r * D + db * 16 + 4 * g) = st.o[qb][db];
+        if (g == 0) *reinterpret_cast<float2*>(part + kTreeShared * D + 2 * r) = float2{st.m[qb], l};
       }
+    }
+  }
 }
 
 // The same for many rows (trees of drafted tokens): up to 256 rows to a group, so that K and V are read once for all of
