@@ -18,8 +18,8 @@ constexpr int kTreeMinRun = kTreeStart + 8;  // a workgroup takes at least so mu
 constexpr int kSharedStart = 24, kSharedMinRun = 36, kSharedNarrow = 3, kSharedWide = 4;
 // Launches whose runs of wide groups (256 rows) would cost less than this are dealt as narrow ones (128): more groups, so
 // fewer are split, for reading the keys of sequences with more rows again. 16 requests of 64 tokens x 4 heads: over 1,000
-// positions 37 us for 50, over 8,000 184 for 167.
-constexpr int kSharedShortRun = 120;
+// positions 39 us for 54, over 8,000 184 for 167; trees of up to 48 tokens over 16 contexts, near the limit, 81 for 84.
+constexpr int kSharedShortRun = 70;
 constexpr int kTreeMaxGroup = 1024;          // query heads of a K/V head
 
 #ifndef SRA_HD

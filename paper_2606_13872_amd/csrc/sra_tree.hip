@@ -19,9 +19,10 @@
 // TB/s of algorithmic bytes, no other bytes fetched; two of 120 to 131 thousand 191 us (5.4 TB/s); four of 31 to 1,500
 // 12 us, a chain of latencies: launch, bounds 1.2 us, first loads 2.5, two chunks 2.5, merge 1, and another 4 us for the
 // second kernel. 64 head dims read 4.4 TB/s (half as long rows); from a cache of a few pages (L2) the kernel takes half
-// the time. Trees of up to 48 tokens over 16 contexts, 40 query heads, both kernels: 68 us (each 32 rows alone
-// with their keys 226, shared tiles without the software pipeline 125, 256 rows to every group 80); 64 tokens each over
-// 16 x 16,384 positions 307 us, 890 TFLOP/s.
+// the time. Trees of up to 48 tokens over 16 contexts, 40 query heads, both kernels: 82 us, 70 where
+// the last-level cache holds the keys (each 32 rows alone with their keys 226, shared tiles without the software pipeline
+// 125, 32 rows to every wave 80); 64 tokens each over 16 x 16,384 positions 307 us, 890 TFLOP/s. A fourth pair of
+// buffers, with the loads two tiles ahead instead of one, gained nothing there and cost 2 to 10 % in short launches.
 #include "sra_fwd_pipe.h"
 #include "sra_tree.h"
 
