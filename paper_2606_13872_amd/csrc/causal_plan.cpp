@@ -4,12 +4,13 @@
 // short ones fill the compute units that long ones leave (a causal prompt's items differ by as much as its
 // length). K/V heads are innermost: item i runs on XCD i % 8, so with 8 heads (or a multiple, or 1, 2, 4) an XCD
 // streams the K and V of one of them through its L2. Where a launch has few, long items, they are cut into
-// pieces whose partial sums a second kernel adds up: the launch is replayed on 256 compute units for a few
+// pieces whose partial sums a second kernel adds up: the launch is replayed on 256 compute units for a few sizes and
 // lengths of the pieces and the one that ends first is taken.
 #include "sra_causal.h"
 
 #include <algorithm>
 #include <functional>
+#include <limits>
 
 namespace sra {
 
@@ -30,17 +31,17 @@ constexpr Cost kForwardCost = {1.0, 5.9, 1.7, 2.75, 0.009};    // 256 rows
 // A step of a large item (384 or 512 rows) to one of 256 rows: 0.93 times the work's share.
 constexpr double large_step(int head_dim) { return 0.93 * fwd_large_tile(head_dim) / kCausalTile; }
 constexpr int kSmallTile = kCausalTile / 2;
-// Backward, in forward steps of a launch that power bounds (1.75 us): a dQ step computes three products to the
-// forward's two, a dK/dV step four. Steps of 64 head dims take 0.6 times as long, what does not depend on them is
-// worth more of them.
-constexpr double kFixed64 = 1.7;
-constexpr Cost backward_cost(CausalKind kind, int head_dim) {
-  const double f = head_dim == 128 ? 1.0 : kFixed64;
-  return kind == kDq ? Cost{1.5, 4.5 * f, 2.2 * f, 3.0 * f, 0.025} : Cost{1.85, 6.0 * f, 4.5 * f, 3.0 * f, 0.05};
-}
+// Backward, in the same way (1.75 and 1.05 us): a dQ step computes three products to the forward's two, a dK/dV step
+// four. Fitted with pairs of 256 and 128 keys and rows: 2 to 3 % slower than the best on average.
+constexpr Cost kDkvCost = {1.77, 7.2, 4.3, 1.5, 0.012}, kSmallDkv = {1.75, 5.5, 2.2, 1.5, 0.012};
+constexpr Cost kDqCost = {1.2, 8.8, 1.8, 1.5, 0.006}, kSmallDq = {1.14, 5.4, 0.9, 1.5, 0.006};
 constexpr int kMaxSplit = 32;
 constexpr size_t kSplitItems = 2048;   // launches of more items are not cut (eight rounds of 256)
+// Launches of 256 rows or keys that end later are not tried with 128: what they may gain (1 to 3 %) is less than planning
+// them costs a caller who has other lengths in each step.
+constexpr double kSmallEnd = 128;
 
+// An item of K/V head 0, uncut; those of the other heads are like it.
 struct Unit {
   CausalItem it;
   int32_t steps;
@@ -54,77 +55,82 @@ int pieces_of(const Unit& u, double cap) {
   return std::min({n, kMaxSplit, u.steps / 2});
 }
 
-// When the last of the launch's pieces ends, launched longest first on 256 compute units.
-double replay(const std::vector<Unit>& units, double cap) {
+// When the last of the launch's pieces ends, launched longest first on 256 compute units; `limit` if not before that.
+double replay(const std::vector<Unit>& units, int32_t heads, double cap, double limit) {
   std::vector<double> c;
   c.reserve(units.size() * 2);
-  double combine = 0, parts = 0;
+  double combine = 0, sum = 0;
   for (const Unit& u : units) {
     const int n = pieces_of(u, cap);
-    if (n > 1) {
-      combine = u.each->combine;
-      parts += n * u.each->part;
-    }
+    if (n > 1) combine = std::max(combine, u.each->combine);
     for (int i = 0; i < n; ++i) {
       const int steps = u.steps * (i + 1) / n - u.steps * i / n;
       c.push_back(u.each->item + steps * u.each->step + (n > 1 ? u.each->slot : 0.0));
+      sum += c.back();
     }
+    if (n > 1) combine += n * u.each->part * heads;
   }
+  if (sum * heads / kNumCus + combine >= limit) return limit;
   std::sort(c.begin(), c.end(), std::greater<double>());
   double heap[kNumCus] = {};  // when each compute unit is free; the first is the least
   double end = 0;
-  for (double x : c) {
-    const double t = heap[0] + x;
-    int i = 0;
-    for (int k; (k = 2 * i + 1) < kNumCus; i = k) {
-      if (k + 1 < kNumCus && heap[k + 1] < heap[k]) ++k;
-      if (heap[k] >= t) break;
-      heap[i] = heap[k];
+  for (double x : c)
+    for (int32_t h = 0; h < heads; ++h) {
+      const double t = heap[0] + x;
+      int i = 0;
+      for (int k; (k = 2 * i + 1) < kNumCus; i = k) {
+        if (k + 1 < kNumCus && heap[k + 1] < heap[k]) ++k;
+        if (heap[k] >= t) break;
+        heap[i] = heap[k];
+      }
+      heap[i] = t;
+      end = std::max(end, t);
     }
-    heap[i] = t;
-    end = std::max(end, t);
-  }
-  return end + combine + parts;
+  return std::min(end + combine, limit);
 }
 
-// The cost from which on items are cut (0: none is), and when the launch then ends.
-double choose_cap(const std::vector<Unit>& units, double* end) {
-  double total = 0;
-  for (const Unit& u : units) total += u.cost();
-  double best_cap = 0, best = replay(units, 0);
-  for (double f : {2.0, 1.5, 1.2, 1.1, 1.0, 0.8, 0.65, 0.5, 0.35}) {
-    const double cap = std::max(f * total / kNumCus, 4.0);
-    const double t = replay(units, cap);
-    if (t < 0.97 * best) best = t, best_cap = cap;
-  }
-  if (end) *end = best;
-  return best_cap;
+// Sets `cap`, the cost from which on items are cut (0: none is), and `end`, when the launch then ends, if that is
+// before *end.
+bool choose_cap(const std::vector<Unit>& units, int32_t heads, double* cap, double* end) {
+  double total = 0, best = *end;
+  for (const Unit& u : units) total += heads * u.cost();
+  auto consider = [&](double c, double least) {
+    const double t = replay(units, heads, c, least * best);
+    if (t < least * best) best = t, *cap = c;
+  };
+  consider(0, 1.0);
+  for (double f : {2.0, 1.5, 1.2, 1.1, 1.0, 0.8, 0.65, 0.5, 0.35}) consider(std::max(f * total / kNumCus, 4.0), 0.97);
+  const bool better = best < *end;
+  *end = best;
+  return better;
 }
 
 // Appends the units' items, cut where `cap` says, longest first.
-void emit(const std::vector<Unit>& units, double cap, std::vector<CausalItem>* items,
+void emit(const std::vector<Unit>& units, int32_t heads, double cap, std::vector<CausalItem>* items,
           std::vector<CausalItem>* combine, int32_t slots[3]) {
   std::vector<std::pair<double, CausalItem>> out;
   for (const Unit& u : units) {
     const int n = pieces_of(u, cap);
-    if (n > 1) {
-      CausalItem c = u.it;
-      c.lo = slots[u.it.kind];
-      c.hi = n;
-      combine->push_back(c);
-    }
-    for (int i = 0; i < n; ++i) {
-      CausalItem x = u.it;
-      const int a = u.steps * i / n, b = u.steps * (i + 1) / n;
-      if (u.it.kind == kDkv) {
-        x.lo = a;
-        x.hi = b;
-      } else {
-        x.lo = 64 * a;
-        x.hi = std::min(64 * b, u.it.hi);
+    CausalItem c = u.it;
+    for (c.kvh = 0; c.kvh < heads; ++c.kvh) {
+      if (n > 1) {
+        c.lo = slots[c.kind];
+        c.hi = n;
+        combine->push_back(c);
       }
-      if (n > 1) x.slot = ++slots[u.it.kind];
-      out.emplace_back((b - a) * u.each->step, x);
+      for (int i = 0; i < n; ++i) {
+        CausalItem x = c;
+        const int a = u.steps * i / n, b = u.steps * (i + 1) / n;
+        if (c.kind == kDkv) {
+          x.lo = a;
+          x.hi = b;
+        } else {
+          x.lo = 64 * a;
+          x.hi = std::min(64 * b, u.it.hi);
+        }
+        if (n > 1) x.slot = ++slots[c.kind];
+        out.emplace_back((b - a) * u.each->step, x);
+      }
     }
   }
   std::stable_sort(out.begin(), out.end(), [](const auto& a, const auto& b) { return a.first > b.first; });
@@ -135,7 +141,7 @@ void emit(const std::vector<Unit>& units, double cap, std::vector<CausalItem>* i
 
 void build_causal_tables(CausalTables* t) {
   const int32_t G = t->heads / t->kv_heads;
-  // Items of `tile` rows or keys each, K/V heads innermost.
+  // Items of `tile` rows or keys each.
   auto units = [&](CausalKind kind, int32_t tile, const Cost& each) {
     std::vector<Unit> out;
     int32_t q0 = 0, k0 = 0;
@@ -151,13 +157,15 @@ void build_causal_tables(CausalTables* t) {
           it.hi = std::max(0, (r + it.len - 1) / G + nk - nq + 1);  // keys seen by the last row
           steps = (it.hi + 63) / 64;
         }
-        for (it.kvh = 0; it.kvh < t->kv_heads; ++it.kvh) out.push_back({it, steps, &each});
+        out.push_back({it, steps, &each});
       }
       q0 += nq;
       k0 += nk;
     }
     return out;
   };
+  const int32_t heads = t->kv_heads;
+  auto few = [&](size_t n) { return n * heads <= kSplitItems; };
   int32_t slots[3] = {0, 0, 0};
   Cost large = kForwardCost;
   large.step = large_step(t->head_dim);
@@ -165,30 +173,37 @@ void build_causal_tables(CausalTables* t) {
   double cap = 0;
   // larger items, or items of 256 or 128 rows, cut or not: whichever end first
   std::vector<Unit> less = units(kForward, kCausalTile, kForwardCost);
-  if (less.size() <= kSplitItems) {
-    double end = replay(fwd, 0);
-    auto consider = [&](std::vector<Unit>&& u, int32_t tile) {
-      double at;
-      const double c = choose_cap(u, &at);
-      if (at > end) return;
-      end = at;
-      cap = c;
-      fwd = std::move(u);
-      t->fwd_tile = tile;
-    };
-    consider(std::move(less), kCausalTile);
-    consider(units(kForward, kSmallTile, kSmallForward), kSmallTile);
+  if (few(less.size())) {
+    double end = replay(fwd, heads, 0, std::numeric_limits<double>::infinity());
+    for (int32_t tile : {kCausalTile, kSmallTile}) {
+      if (tile == kSmallTile) {
+        if (end > kSmallEnd) break;
+        less = units(kForward, kSmallTile, kSmallForward);
+      }
+      if (choose_cap(less, heads, &cap, &end)) {
+        fwd = std::move(less);
+        t->fwd_tile = tile;
+      }
+    }
   }
-  emit(fwd, cap, &t->fwd, &t->fwd_combine, slots);
+  emit(fwd, heads, cap, &t->fwd, &t->fwd_combine, slots);
   if (t->backward) {
-    const Cost dkv_cost = backward_cost(kDkv, t->head_dim), dq_cost = backward_cost(kDq, t->head_dim);
-    std::vector<Unit> dkv = units(kDkv, kCausalTile, dkv_cost), dq = units(kDq, kCausalTile, dq_cost);
-    if (dq.size() + dkv.size() <= kSplitItems) {  // few items: both kinds together, each fills the other's gaps
-      dkv.insert(dkv.end(), dq.begin(), dq.end());
-      emit(dkv, choose_cap(dkv, nullptr), &t->grad, &t->grad_combine, slots);
+    std::vector<Unit> dkv = units(kDkv, kCausalTile, kDkvCost), dq = units(kDq, kCausalTile, kDqCost);
+    if (few(dq.size() + dkv.size())) {  // both kinds together, each fills the other's gaps
+      std::vector<Unit> best;
+      double end = std::numeric_limits<double>::infinity();
+      for (int i = 0; i < 3; ++i) {  // items of 256 or 128, cut or not: whichever end first
+        if (i > 0 && end > kSmallEnd) break;
+        if (i == 1) dkv = units(kDkv, kSmallTile, kSmallDkv);
+        if (i == 2) dq = units(kDq, kSmallTile, kSmallDq);
+        std::vector<Unit> both = dkv;
+        both.insert(both.end(), dq.begin(), dq.end());
+        if (choose_cap(both, heads, &cap, &end)) best = std::move(both);
+      }
+      emit(best, heads, cap, &t->grad, &t->grad_combine, slots);
     } else {  // many: one kind after the other, so that an XCD streams one kind of rows at a time
-      emit(dkv, 0, &t->grad, &t->grad_combine, slots);
-      emit(dq, 0, &t->grad, &t->grad_combine, slots);
+      emit(dkv, heads, 0, &t->grad, &t->grad_combine, slots);
+      emit(dq, heads, 0, &t->grad, &t->grad_combine, slots);
     }
   }
   t->fwd_slots = slots[kForward];
