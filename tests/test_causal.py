@@ -178,3 +178,28 @@ def test_largest_plans():
     p = sra.CausalPlan([1], 1, 1, 64, k_lens=[2**28 - 1])
     assert p.n_k == 2**28 - 1 and p.backward_workspace > 0
     assert sra.CausalPlan([2**18 - 1], 1, 1, 128, k_lens=[1], backward=False).n_q == 2**18 - 1
+
+
+def _longest_items(plan):
+    """Rows or keys of the longest item of each kind in the plan's tables (records of 12 int32, sections 256-byte aligned)."""
+    t = np.zeros(plan._table_bytes, dtype=np.uint8)
+    assert binding._lib().sra_causal_plan_tables(plan._handle, t.ctypes.data, plan._table_bytes) == 0
+    r, at, longest = t.view(np.int32), 0, {0: 0, 1: 0, 2: 0}
+    while at + 12 <= len(r):
+        if r[at + 3] > 0:
+            longest[int(r[at])] = max(longest[int(r[at])], int(r[at + 3]))
+            at += 12
+        else:
+            at = (at // 64 + 1) * 64
+    return longest
+
+
+@pytest.mark.parametrize("lens,heads,kv,d,forward,cut,backward", [
+    ([700], 4, 2, 128, 128, False, 128), ([2500, 311], 2, 2, 64, 128, True, 256), ([2000, 1900, 300], 24, 8, 128, 256, False, 256),
+    ([1500, 200, 900] * 3, 16, 8, 64, 256, False, 256), ([4099], 4, 1, 128, 256, True, 256), ([4099], 4, 1, 64, 256, True, 256),
+    ([1500, 200, 900] * 3, 16, 8, 128, 384, False, 256), ([9000] * 2, 32, 8, 64, 512, False, 256),
+])
+def test_items_grow_with_the_launch(lens, heads, kv, d, forward, cut, backward):
+    p = sra.CausalPlan(lens, heads, kv, d)
+    n = _longest_items(p)
+    assert (n[0], n[1], n[2]) == (forward, backward, backward) and (p.forward_workspace > 0) == cut

@@ -249,3 +249,14 @@ def test_plans_are_made_outside_a_capture():
         with pytest.raises(sra.SRAError, match="capture"):
             sra.CausalPlan([5], 4, 2, 64)
         x.add_(1)
+
+
+@pytest.mark.parametrize("nq,nk,heads,kv,d", [
+    ([2000, 1900, 300], [2000, 1900, 300], 24, 8, 128), ([1500, 200, 900] * 3, [1500, 200, 900] * 3, 16, 8, 64),
+    ([1500, 200, 900] * 3, [1500, 200, 900] * 3, 16, 8, 128), ([1800, 77, 1100], [2300, 77, 1500], 40, 8, 128),
+    ([2500, 311], [2500, 311], 2, 2, 64),
+])
+def test_launches_between_short_and_long(nq, nk, heads, kv, d):
+    """Items of 256 rows that are not cut, cut ones of 128, and their neighbours."""
+    print("causal middle", nq, heads, kv, d, flush=True)
+    _check(nq, nk, heads, kv, d, seed=40 + heads)
