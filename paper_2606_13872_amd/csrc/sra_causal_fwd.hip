@@ -3,18 +3,21 @@
 //   S = scale Q K^T on the keys j <= i + nk - nq of token i, LSE = ln sum exp S, O = exp(S - LSE) V,
 //
 // one pass over the keys with a running maximum and sum. One workgroup (8 wave64s, two per SIMD) takes one work
-// item (sra_causal.h): up to 256 (token, head of the group) rows, 32 per wave (long launches: 384, or 512 of 64 head
-// dims, which read and load the keys less often), against the keys up to the last that its rows see. The key tiles
-// that every row sees run through the software pipeline of sra_fwd_pipe.h; those on the diagonal (256 / G tokens wide)
-// run behind it, three at a time, masked by each row's last key. Rows that see nothing (nq > nk) end with l = 0: O = 0,
-// LSE = -inf. P is rounded to bf16 for the matrix product; its sum, the maxima and O stay in 32 bits.
+// item (sra_causal.h): up to 256 (token, head of the group) rows, 32 per wave (short launches: 128, for more and shorter
+// items; long ones: 384, or 512 of 64 head dims, which read and load the keys less often), against the keys up to the
+// last that its rows see. The key tiles that every row sees run through the software pipeline of sra_fwd_pipe.h; those
+// on the diagonal (256 / G tokens wide) run behind it, three at a time, masked by each row's last key. Rows that see
+// nothing (nq > nk) end with l = 0: O = 0, LSE = -inf. P is rounded to bf16 for the matrix product; its sum, the maxima
+// and O stay in 32 bits.
 //
 // Long launches are bound by the clock that the board's power allows (1.88 of 2.4 GHz, MFMA pipes busy 65 % of the
-// cycles): 32,768 tokens, 32 query and 8 K/V heads of 128 dims 6.75 -> 6.28 ms (1,400 TFLOP/s) with 384 rows for
-// 256. Short ones by the chain of an item: about 5 us for its loads, diagonal and epilogue and 1.75 us a step of 64 keys
-// (64 head dims: 1.1 us, the exponentials alone). Running the diagonal through the pipeline too, with masked blocks, was
-// 1 to 2 % slower on every size (more vector work per MFMA, twice the code), and one loop body with its buffers
-// chosen at run time, instead of three, 3 % on long ones.
+// cycles): 32,768 tokens, 32 query and 8 K/V heads of 128 dims 6.75 -> 6.28 ms (1,400 TFLOP/s; timed in turn)
+// with 384 rows for 256. Short ones by the chain of an item: 6 us (128 rows) to 8 us (256) for its loads, diagonal and epilogue, and 0.9 or
+// 1.4 us a step of 64 keys: 512, 700 and 129 tokens of 16 heads of 64 dims 19.3 -> 12.5 us with 128 rows for 256, 512
+// tokens of 8 heads of 128 dims 23.6 -> 14.0. Loading the first diagonal tile within the pipeline gained nothing (1.5 %
+// slower: more code). Running the diagonal through the pipeline too, with masked blocks, was 1 to 2 % slower on every
+// size (more vector work per MFMA, twice the code), and one loop body with its buffers chosen at run time, instead of
+// three, 3 % on long ones.
 #include <type_traits>
 
 #include "sra_causal_kernels.h"
@@ -226,8 +229,8 @@ sra_causal_fwd_kernel(CausalArgs a) {
 }
 
 // Rows of the split items from their pieces, in piece order: with M the largest of the pieces' running maxima,
-// O = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i. D / 4 threads per row. Bound by reading the partial results (25 MB: 8.5 us;
-// with the maxima in a pass of their own 15 us).
+// O = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i. D / 4 threads per row. Bound by reading the partial results (25 MB:
+// 8.5 us; with the maxima in a pass of their own 15 us).
 template <int D>
 __global__ void __launch_bounds__(kThreads) sra_causal_fwd_combine_kernel(CausalArgs a, const CausalItem* items) {
   constexpr int TPR = D / 4, RPB = kThreads / TPR;
