@@ -49,24 +49,26 @@ def _ints(t, name, dims, dtype):
     """An integer tensor of so many dims with contiguous entries."""
     if not isinstance(t, _s._tm().Tensor) or t.dtype != dtype or t.dim() != dims:
         raise _s._bad(f"{name} must be a {dims}-dimensional {dtype} tensor")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+    if not t.is_contiguous() and t.shape[-1] > 1 and t.stride(-1) != 1:
         raise _s._bad(f"{name}: entries must be contiguous")
 
 
 def _pages(t, name, shape, kv_heads, head_dim):
     """Page and token strides of a cache tensor (0: it has one page)."""
     torch = _s._tm()
-    if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16 or t.dim() != 4:
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16 or len(shape) != 4:
         raise _s._bad(f"{name} must be a bfloat16 [pages, page_size, kv_heads, head_dim] tensor")
-    if t.shape != shape or shape[2] != kv_heads or shape[3] != head_dim:
+    pages, size, heads, dim = shape
+    if t.shape != shape or heads != kv_heads or dim != head_dim:
         raise _s._bad(f"{name}: shape {tuple(t.shape)}, expected [pages, page_size, {kv_heads}, {head_dim}]")
-    st, row = t.stride(), kv_heads * head_dim
-    if shape[0] and shape[1]:
-        if st[3] != 1 or (kv_heads > 1 and st[2] != head_dim):
+    page, token, head, one = t.stride()
+    row = heads * dim
+    if pages and size:
+        if one != 1 or (head != dim and heads > 1):
             raise _s._bad(f"{name} must have contiguous heads")
-        if st[1] < row or (shape[0] > 1 and st[0] < (shape[1] - 1) * st[1] + row):
+        if token < row or (pages > 1 and page < (size - 1) * token + row):
             raise _s._bad(f"{name}: tokens or pages overlap")
-    return st[0] if shape[0] > 1 else 0, st[1]
+    return page if pages > 1 else 0, token
 
 
 def _cache(k_cache, v_cache, page_table, context_lens, cu_tokens, tokens, kv_heads, head_dim):

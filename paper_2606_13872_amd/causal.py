@@ -136,7 +136,8 @@ def _rows(t, name, shape):
 
 
 def _addr(t):
-    return t.data_ptr() if t is not None and t.numel() else None
+    """Its address (None without elements)."""
+    return None if t is None else t.data_ptr() or None
 
 
 def _qkv(q, k, v, plan):

@@ -414,7 +414,7 @@ def _same_device(tensors, device):
         raise _bad(f"tensors must be on a GPU (HIP device), got {device}")
     idx = device.index
     for name, t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != idx):
+        if t is not None and t.get_device() != idx:  # -1: on the CPU
             raise _bad(f"{name} is on {t.device}, q_gen on {device}")
 
 
