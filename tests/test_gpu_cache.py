@@ -372,3 +372,11 @@ def test_long_steps_with_groups_of_all_widths(heads, kv, d, page, tree):
         kh, vh = (torch.cat([c[keep, g], x[n][a:b, g]]).double() for c, n in ((k, "k"), (v, "v")))
         want, want_lse, _, eo, el = T.rows(x["q"][a:b, h].double(), kh, vh, see, 1 / math.sqrt(d))
         assert T.within(bad_o[a:b, h], want, eo)[0] and T.within(bad_lse[h, a:b], want_lse, el)[0]
+
+
+@pytest.mark.parametrize("ctx,new,heads", [([100, 5], [70, 1], 8), ([30] * 40 + [100], [1] * 40 + [70], 2)])
+def test_masks_of_more_tokens_than_they_have_bits(ctx, new, heads):
+    """Tokens from the 65th on see the first 64 new ones by their masks, and are seen by none."""
+    print("tree bits", heads, flush=True)
+    x, tree, cu = make(ctx, new, heads, 2, 128, 16, seed=50)
+    check(x, tree, ctx, cu)
