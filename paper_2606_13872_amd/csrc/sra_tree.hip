@@ -19,10 +19,9 @@
 // TB/s of algorithmic bytes, no other bytes fetched; two of 120 to 131 thousand 191 us (5.4 TB/s); four of 31 to 1,500
 // 12 us, a chain of latencies: launch, bounds 1.2 us, first loads 2.5, two chunks 2.5, merge 1, and another 4 us for the
 // second kernel. 64 head dims read 4.4 TB/s (half as long rows); from a cache of a few pages (L2) the kernel takes half
-// the time. Trees of up to 48 tokens over 16 contexts, 40 query heads, both kernels: 82 us, 70 where
-// the last-level cache holds the keys (each 32 rows alone with their keys 226, shared tiles without the software pipeline
-// 125, 32 rows to every wave 80); 64 tokens each over 16 x 16,384 positions 307 us, 890 TFLOP/s. A fourth pair of
-// buffers, with the loads two tiles ahead instead of one, gained nothing there and cost 2 to 10 % in short launches.
+// the time. Trees of up to 48 tokens over 16 contexts, 40 query heads, both kernels: 82 us, 70 where the last-level
+// cache holds the keys (each 32 rows alone with their keys 226, shared tiles without the software pipeline 125, 32 rows
+// to every wave 80); 64 tokens each over 16 x 16,384 positions 307 us, 890 TFLOP/s.
 #include "sra_fwd_pipe.h"
 #include "sra_tree.h"
 
@@ -32,6 +31,10 @@ namespace {
 constexpr int kTreeWaves = 4;
 constexpr int kTreeThreads = kTreeWaves * 64;
 constexpr int kSharedChunk = 64;
+// LDS buffers of the shared kernel, for K and for V. Four, with loads two tiles ahead that a tile's end does not wait for:
+// 64 requests of 4,000 positions and 16 tokens, 64 head dims, 134 -> 115 us; groups of more rows 3 % slower, and 128 head
+// dims spill for them.
+template <int D, int NQ> constexpr int kTileBufs = D == 64 && NQ == 1 ? 4 : 3;
 constexpr int kNarrow = 128;  // rows of a narrow group of the shared kernel: 16 per wave
 // Costs by C, the keys of a chunk: of beginning a group, of a chunk of a narrow and of a wide group, and of the least run.
 template <int C> constexpr int kStart = C == kSharedChunk ? kSharedStart : kTreeStart;
@@ -580,19 +583,22 @@ __device__ __forceinline__ void tree_half(FwdState<D, NQ>& st, const __bf16* kt,
 }
 
 // Where the shared kernel's tiles lie.
+template <int D>
 struct SharedTiles {
-  __bf16 *k[3], *v[3];
+  __bf16 *k[kTileBufs<D, 1>], *v[kTileBufs<D, 1>];
 };
 
 // The run's share of a group of at most 128 NQ rows, 16 NQ per wave; an unfinished group's results go to `part`.
 template <int D, int NQ>
-__device__ __forceinline__ void shared_group(const TreeArgs& a, const TreeSegment& seg, const SharedTiles& lds, float* part) {
+__device__ __forceinline__ void shared_group(const TreeArgs& a, const TreeSegment& seg, const SharedTiles<D>& lds,
+                                             float* part) {
   constexpr int NC = D / 32, ND = D / 16, C = kSharedChunk;
   using TL = SwzTile<D, C>;
   constexpr int RPI = 512 / D, CPR = D / 8, kPer = TL::kInstr / kWaves;  // rows of a load instruction; a wave's of a tile
   static_assert(kPer >= 1 && RPI * kWaves % 8 == 0 && C == kFwdKeyStep, "tiles by waves");
-  __bf16* const kb[3] = {lds.k[0], lds.k[1], lds.k[2]};
-  __bf16* const vb[3] = {lds.v[0], lds.v[1], lds.v[2]};
+  constexpr int NB = kTileBufs<D, NQ>;
+  __bf16* const* const kb = lds.k;
+  __bf16* const* const vb = lds.v;
   const PagedCache& c = a.c;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int g = lane >> 4, l16 = lane & 15;
@@ -647,6 +653,10 @@ __device__ __forceinline__ void shared_group(const TreeArgs& a, const TreeSegmen
     issue_k(kb[0]);
     issue_v(vb[0]);
     if (T > 1) issue_k(kb[1]);
+    if constexpr (NB == 4) {
+      if (T > 1) issue_v(vb[1]);
+      if (T > 2) issue_k(kb[2]);
+    }
   }
 
   FwdState<D, NQ> st;
@@ -671,11 +681,11 @@ __device__ __forceinline__ void shared_group(const TreeArgs& a, const TreeSegmen
 #pragma unroll
     for (int i = 0; i < NC; ++i) asm volatile("" : "+v"(st.qf[qb][i]));
 
-  // Tile t sits in K buffer t % 3 and V buffer t % 3 (tile -1 in V buffer 2). Iteration t reads K(t) (second half),
-  // K(t+1) (first half), V(t-1) (second half) and V(t) (first half), and loads K(t+2) and V(t+1).
+  // Tile t sits in K buffer t % NB and V buffer t % NB (tile -1 in V buffer NB - 1). Iteration t reads K(t) (second
+  // half), K(t+1) (first half), V(t-1) (second half) and V(t) (first half), and loads K(t+NB-1) and V(t+NB-2).
   if (T > 0) {
     for (int e = threadIdx.x * 8; e < 32 * D; e += kWaves * 64 * 8)
-      *reinterpret_cast<bf16x8*>(vb[2] + 32 * D + e) = bf16x8{};
+      *reinterpret_cast<bf16x8*>(vb[NB - 1] + 32 * D + e) = bf16x8{};
     wait_vmem();
     __syncthreads();
     HalfP<NQ> p_hi;
@@ -687,41 +697,48 @@ __device__ __forceinline__ void shared_group(const TreeArgs& a, const TreeSegmen
 #pragma unroll
     for (int i = 0; i < kLook; ++i) {
       ah.k[i] = k_frag<D, SwizzledRows>(kb[0] + 32 * D, i);
-      ah.v[i] = v_frag<D, SwizzledRows>(vb[2] + 32 * D, i);
+      ah.v[i] = v_frag<D, SwizzledRows>(vb[NB - 1] + 32 * D, i);
     }
     auto iteration = [&](int t, auto phase) {
       constexpr int P = decltype(phase)::value;
       __bf16* const k_t = kb[P];
-      __bf16* const k_t1 = kb[(P + 1) % 3];
-      __bf16* const v_tm1 = vb[(P + 2) % 3];
+      __bf16* const k_t1 = kb[(P + 1) % NB];
+      __bf16* const v_tm1 = vb[(P + NB - 1) % NB];
       __bf16* const v_t = vb[P];
-      if (t + 1 < T) issue_v(vb[(P + 1) % 3]);
-      if (t + 2 < T) issue_k(kb[(P + 2) % 3]);
+      if (t + NB - 2 < T) issue_v(vb[(P + NB - 2) % NB]);
+      if (t + NB - 1 < T) issue_k(kb[(P + NB - 1) % NB]);
       if (active) {
         const HalfP<NQ> p_lo = pipe_block<D, NQ, SwizzledRows>(st, s_lo, k_t, s_hi, k_t + 32 * D, v_tm1 + 32 * D, k_t1,
                                                                v_t, ah, p_hi, sl2);
         p_hi = pipe_block<D, NQ, SwizzledRows>(st, s_hi, k_t + 32 * D, s_lo, k_t1, v_t, k_t1 + 32 * D, v_t + 32 * D, ah,
                                                p_lo, sl2);
       }
-      wait_vmem();
+      // with four buffers this iteration's loads may be in flight
+      if (NB == 4 && t + NB - 1 < T) wait_vmem_to<2 * kPer>();
+      else wait_vmem();
       __syncthreads();
     };
     using P0 = std::integral_constant<int, 0>;
     using P1 = std::integral_constant<int, 1>;
     using P2 = std::integral_constant<int, 2>;
+    using P3 = std::integral_constant<int, 3>;
     int t = 0;
-    for (; t + 3 <= T; t += 3) {
+    for (; t + NB <= T; t += NB) {
       iteration(t, P0{});
       iteration(t + 1, P1{});
       iteration(t + 2, P2{});
+      if constexpr (NB == 4) iteration(t + 3, P3{});
     }
     if (t < T) iteration(t, P0{});
     if (t + 1 < T) iteration(t + 1, P1{});
+    if constexpr (NB == 4)
+      if (t + 2 < T) iteration(t + 2, P2{});
     if (active) {
-      const int last = (T - 1) % 3;
+      const int last = (T - 1) % NB;
       if (last == 0) pv_half<D, NQ, SwizzledRows>(st, vb[0] + 32 * D, p_hi);
       else if (last == 1) pv_half<D, NQ, SwizzledRows>(st, vb[1] + 32 * D, p_hi);
-      else pv_half<D, NQ, SwizzledRows>(st, vb[2] + 32 * D, p_hi);
+      else if (NB == 3 || last == 2) pv_half<D, NQ, SwizzledRows>(st, vb[2] + 32 * D, p_hi);
+      else pv_half<D, NQ, SwizzledRows>(st, vb[NB - 1] + 32 * D, p_hi);
     }
   }
 
@@ -790,20 +807,25 @@ __device__ __forceinline__ void shared_group(const TreeArgs& a, const TreeSegmen
 // the group has up to 128 or more (32 for all of them: half of the waves idle, 6 % slower); the keys go through LDS in
 // 64-key tiles that all of them read.
 // Whole tiles of the context run through the software pipeline of sra_fwd_pipe.h (three buffers each for K and V, loads
-// two and one tiles ahead), the context's end and the new tokens behind them, masked. Where the table names a page
+// two and one tiles ahead, or four), the context's end and the new tokens behind them, masked. Where the table names a page
 // that is none, all of the group's tiles run masked.
 template <int D>
 __global__ void __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 sra_tree_shared_kernel(TreeArgs a) {
   constexpr int C = kSharedChunk;
   using TL = SwzTile<D, C>;
+  constexpr int NB = kTileBufs<D, 1>;
   __shared__ __attribute__((aligned(1024))) __bf16 kbuf0[TL::kElems];
   __shared__ __attribute__((aligned(1024))) __bf16 kbuf1[TL::kElems];
   __shared__ __attribute__((aligned(1024))) __bf16 kbuf2[TL::kElems];
   __shared__ __attribute__((aligned(1024))) __bf16 vbuf0[TL::kElems];
   __shared__ __attribute__((aligned(1024))) __bf16 vbuf1[TL::kElems];
   __shared__ __attribute__((aligned(1024))) __bf16 vbuf2[TL::kElems];
-  const SharedTiles tiles{{kbuf0, kbuf1, kbuf2}, {vbuf0, vbuf1, vbuf2}};
+  __shared__ __attribute__((aligned(1024))) __bf16 buf3[NB == 4 ? 2 * TL::kElems : 8];
+  SharedTiles<D> tiles;
+  tiles.k[0] = kbuf0, tiles.k[1] = kbuf1, tiles.k[2] = kbuf2;
+  tiles.v[0] = vbuf0, tiles.v[1] = vbuf1, tiles.v[2] = vbuf2;
+  if constexpr (NB == 4) tiles.k[3] = buf3, tiles.v[3] = buf3 + TL::kElems;
   __shared__ TreeBounds<2> bounds;
   const PagedCache& c = a.c;
   const int G = a.heads / c.kv_heads;
