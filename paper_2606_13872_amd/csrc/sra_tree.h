@@ -30,6 +30,13 @@ constexpr int kTreeMaxGroup = 1024;          // query heads of a K/V head
 #endif
 #endif
 
+// What each workgroup takes of a launch that costs `total` in all (up to 2^31 - 1, so rounded up without adding to it), at
+// least `least`.
+SRA_HD inline int32_t tree_run(int32_t total, int32_t least) {
+  const int32_t run = total / kTreeGroups + (total % kTreeGroups != 0);
+  return run > least ? run : least;
+}
+
 // A group of rows whose keys were split over workgroups, written by the one (w) that has its first keys. That piece is
 // in slot 2 w + 1, the others, with which their workgroups begin, in slots 2 (w + i).
 struct TreeSplit {

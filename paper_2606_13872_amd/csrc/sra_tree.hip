@@ -369,7 +369,7 @@ __global__ void __launch_bounds__(kTreeThreads) sra_tree_kernel(TreeArgs a) {
 
   tree_bounds<R, kTreeChunk>(a, bounds);
   const int total = __builtin_amdgcn_readfirstlane(bounds.cost[0][c.batch]);
-  const int run = max(kMinRun<kTreeChunk>, (total + kTreeGroups - 1) / kTreeGroups);
+  const int run = tree_run(total, kMinRun<kTreeChunk>);
   const int begin = int(min(int64_t(w) * run, int64_t(total))), end = int(min(int64_t(begin) + run, int64_t(total)));
   TreeSplit split{0, 0, 0, 0, 0};
 
@@ -838,7 +838,7 @@ sra_tree_shared_kernel(TreeArgs a) {
     deal = 1;
     total = __builtin_amdgcn_readfirstlane(bounds.cost[1][c.batch]);
   }
-  const int run = max(kMinRun<C>, (total + kTreeGroups - 1) / kTreeGroups);
+  const int run = tree_run(total, kMinRun<C>);
   const int begin = int(min(int64_t(w) * run, int64_t(total))), end = int(min(int64_t(begin) + run, int64_t(total)));
   TreeSplit split{0, 0, 0, 0, 0};
   for (int x = begin; x < end;) {
