@@ -53,6 +53,10 @@ def _lens(x, name) -> np.ndarray:
     return np.ascontiguousarray(a.astype(np.int32))
 
 
+class _PlanHandle(ctypes.c_void_p):
+    """An sra_causal_plan, destroyed with the last object that holds it (copies of a CausalPlan share it)."""
+
+
 class CausalPlan:
     """The tile schedule of causal attention for one set of lengths, with its tables on `device` (default: the
     current GPU; without a GPU only the host hooks work). Made once, used by every layer and call with these lengths.
@@ -72,10 +76,10 @@ class CausalPlan:
         self.heads, self.kv_heads, self.head_dim, self.backward = int(heads), int(kv_heads), int(head_dim), bool(backward)
         p = _CausalProblem(len(self.q_lens), self.heads, self.kv_heads, self.head_dim, self.q_lens.ctypes.data,
                            self.k_lens.ctypes.data)
-        h = ctypes.c_void_p()
+        h = _PlanHandle()
         _s._check(L.sra_causal_plan_create(ctypes.byref(p), 1 if backward else 0, ctypes.byref(h)))
+        weakref.finalize(h, L.sra_causal_plan_destroy, h.value)
         self._handle = h
-        self._finalizer = weakref.finalize(self, L.sra_causal_plan_destroy, h)
         t, f, b = ctypes.c_size_t(), ctypes.c_size_t(), ctypes.c_size_t()
         _s._check(L.sra_causal_plan_sizes(h, ctypes.byref(t), ctypes.byref(f), ctypes.byref(b)))
         self._table_bytes, self.forward_workspace, self.backward_workspace = t.value, f.value, b.value
