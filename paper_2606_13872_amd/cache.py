@@ -12,7 +12,7 @@ from typing import Dict, Optional
 import numpy as np
 
 from . import sra as _s
-from .causal import _addr, _call, _no_alias, _rows
+from .causal import INT32_MAX, _addr, _call, _no_alias, _rows
 
 _declared = False
 
@@ -86,6 +86,8 @@ def _cache(k_cache, v_cache, page_table, context_lens, cu_tokens, tokens, kv_hea
     rows, width = page_table.shape
     if rows != n or cu_tokens.shape[0] != n + 1:
         raise _s._bad("page_table needs one row and cu_tokens one entry more than context_lens has")
+    if max(n, tokens, width, *shape[:2]) > INT32_MAX:
+        raise _s._bad("sequences, tokens, pages, page_size and page_table entries must be below 2^31")
     ts = page_table.stride(0) if n > 1 else 0
     if n > 1 and ts < width:
         raise _s._bad("page_table: rows overlap")

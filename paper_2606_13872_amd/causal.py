@@ -14,6 +14,8 @@ import numpy as np
 
 from . import sra as _s
 
+INT32_MAX = 2**31 - 1  # sizes reach the library in 32 bits, which ctypes would cut them to
+
 _handles_declared = False
 
 
@@ -48,7 +50,7 @@ def _lens(x, name) -> np.ndarray:
     a = np.asarray(x.detach().cpu() if hasattr(x, "detach") else x)
     if a.ndim != 1 or a.size == 0 or a.dtype.kind not in "iu":
         raise _s._bad(f"{name} must be a non-empty sequence of integers")
-    if a.min() < 0 or a.max() > 2**31 - 1:
+    if a.min() < 0 or a.max() > INT32_MAX:
         raise _s._bad(f"{name}: lengths must be between 0 and 2^31 - 1")
     return np.ascontiguousarray(a.astype(np.int32))
 
@@ -74,6 +76,8 @@ class CausalPlan:
         if self.k_lens.shape != self.q_lens.shape:
             raise _s._bad("q_lens and k_lens must have one length per sequence each")
         self.heads, self.kv_heads, self.head_dim, self.backward = int(heads), int(kv_heads), int(head_dim), bool(backward)
+        if max(len(self.q_lens), abs(self.heads), abs(self.kv_heads), abs(self.head_dim)) > INT32_MAX:
+            raise _s._bad("sequences, heads and head_dim must be below 2^31")
         p = _CausalProblem(len(self.q_lens), self.heads, self.kv_heads, self.head_dim, self.q_lens.ctypes.data,
                            self.k_lens.ctypes.data)
         h = _PlanHandle()

@@ -3,6 +3,10 @@ import ctypes
 import os
 import subprocess
 
+import pytest
+import torch
+
+import paper_2606_13872_amd as sra
 from paper_2606_13872_amd import build
 from paper_2606_13872_amd import cache as binding
 
@@ -35,3 +39,15 @@ def test_runs_cover_the_largest_launch_that_is_accepted(tmp_path):
         for least in (16, 36):
             run = L.run(t, least)
             assert run >= least and run * n >= t and (run == least or (run - 1) * n < t), (t, least, run)
+
+
+@pytest.mark.parametrize("tokens,width,batch", [(2**32 + 5, 3, 1), (5, 2**32 + 1, 1), (5, 3, 2**32 + 1), (2**31, 3, 1)])
+def test_sizes_past_32_bits_are_refused(tokens, width, batch):
+    """They would reach the library cut to their lower 32 bits."""
+    def ints(*shape):
+        return torch.empty(shape, dtype=torch.int32, device="meta")
+
+    cache = torch.empty(6, 8, 2, 64, dtype=torch.bfloat16, device="meta")
+    with pytest.raises(sra.SRAError) as e:
+        binding._cache(cache, cache, ints(batch, width), ints(batch), ints(batch + 1), tokens, 2, 64)
+    assert e.value.status == 1

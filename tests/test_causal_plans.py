@@ -4,6 +4,8 @@ import gc
 import weakref
 
 import numpy as np
+import pytest
+
 import paper_2606_13872_amd as sra
 
 
@@ -21,3 +23,11 @@ def test_a_copied_plan_outlives_the_first():
     del other
     gc.collect()
     assert held() is None
+
+
+@pytest.mark.parametrize("sizes", [(2**32 + 8, 2, 64), (8, 2**32 + 2, 64), (8, 2, 2**32 + 64), (-2**32 + 8, 2, 64)])
+def test_sizes_past_32_bits_are_refused(sizes):
+    """They would reach the library cut to their lower 32 bits."""
+    with pytest.raises(sra.SRAError) as e:
+        sra.CausalPlan([3], *sizes)
+    assert e.value.status == 1
