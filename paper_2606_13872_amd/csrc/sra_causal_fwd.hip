@@ -12,12 +12,12 @@
 //
 // Long launches are bound by the clock that the board's power allows (1.88 of 2.4 GHz, MFMA pipes busy 65 % of the
 // cycles): 32,768 tokens, 32 query and 8 K/V heads of 128 dims 6.75 -> 6.28 ms (1,400 TFLOP/s; timed in turn)
-// with 384 rows for 256. Short ones by the chain of an item: 6 us (128 rows) to 8 us (256) for its loads, diagonal and epilogue, and 0.9 or
-// 1.4 us a step of 64 keys: 512, 700 and 129 tokens of 16 heads of 64 dims 19.3 -> 12.5 us with 128 rows for 256, 512
-// tokens of 8 heads of 128 dims 23.6 -> 14.0. Loading the first diagonal tile within the pipeline gained nothing (1.5 %
-// slower: more code). Running the diagonal through the pipeline too, with masked blocks, was 1 to 2 % slower on every
-// size (more vector work per MFMA, twice the code), and one loop body with its buffers chosen at run time, instead of
-// three, 3 % on long ones.
+// with 384 rows for 256. Short ones by the chain of an item: 6 us (128 rows) to 8 us (256) for its loads, diagonal and
+// epilogue, and 0.9 or 1.4 us a step of 64 keys: 512, 700 and 129 tokens of 16 heads of 64 dims 19.3 -> 12.5 us with 128
+// rows for 256, 512 tokens of 8 heads of 128 dims 23.6 -> 14.0. Loading the first diagonal tile within the pipeline gained
+// nothing (1.5 % slower: more code). Running the diagonal through the pipeline too, with masked blocks, was 1 to 2 %
+// slower on every size (more vector work per MFMA, twice the code), and one loop body with its buffers chosen at run time,
+// instead of three, 3 % on long ones.
 #include <type_traits>
 
 #include "sra_causal_kernels.h"

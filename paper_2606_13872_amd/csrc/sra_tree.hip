@@ -774,7 +774,7 @@ __device__ __forceinline__ void shared_group(const TreeArgs& a, const TreeSegmen
   }
 
   const bool whole = c0 == 0 && c1 == n;
-      if (active) {
+  if (active) {
 #pragma unroll
     for (int qb = 0; qb < NQ; ++qb) {
       const int r = wrow + 16 * qb + l16;
