@@ -124,3 +124,43 @@ def test_infinities_and_nan_stay_in_their_sequence(new, heads, d):
             keep = torch.ones(cu[-1], dtype=torch.bool, device="cuda")
             keep[at] = False
             assert torch.equal(got[0][keep], o[keep]) and torch.equal(got[1][:, keep], lse[:, keep]), (b, bad)
+
+
+@pytest.mark.parametrize("heads,kv,d,new", [(1024, 1, 64, [1, 2]), (1000, 1, 64, [3]), (77, 7, 128, [1, 13, 2]), (37, 1, 64, [1, 1, 1])])
+def test_many_heads_of_one_key_head(heads, kv, d, new):
+    """Tokens whose heads take several groups of rows, and groups that begin and end inside a token's heads."""
+    print("wide groups", heads, kv, d, new, flush=True)
+    ctx = [70, 333, 0][:len(new)]
+    x, tree, cu = make(ctx, new, heads, kv, d, 16, seed=100)
+    check(x, tree, ctx, cu)
+
+
+@pytest.mark.parametrize("new", [[1, 1, 1], [9, 30, 20]])
+def test_sequences_that_share_pages_and_pages_larger_than_a_context(new):
+    print("shared pages", new, flush=True)
+    ctx = [200, 640, 513]
+    for page in (32, 1024):
+        x, tree, cu = make(ctx, new, 8, 2, 128, page, seed=110)
+        for n in (1, 2):  # the first positions of all three lie in the first sequence's pages
+            x["page_table"][n, :192 // page] = x["page_table"][0, :192 // page]
+        check(x, tree, ctx, cu)
+
+
+def test_new_tokens_as_views_of_one_projection():
+    """q, k and v of one buffer give what dense copies give, to the attention and to the append."""
+    print("views", flush=True)
+    ctx, new = [60, 0, 200], [3, 40, 1]
+    for d in (64, 128):
+        x, tree, cu = make(ctx, new, 8, 2, d, 16, seed=120)
+        buf = torch.cat([x["q"], x["k"], x["v"]], dim=1)
+        views = {"q": buf[:, :8], "k": buf[:, 8:10], "v": buf[:, 10:]}
+        want = sra.tree_attention(**x, tree=tree)
+        got = sra.tree_attention(**{**x, **views}, tree=tree)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        where = [x[n] for n in ("page_table", "context_lens", "cu_tokens")]
+        caches = [[x[n].clone() for n in ("k_cache", "v_cache")] for _ in range(2)]
+        sra.cache_append(x["k"], x["v"], *caches[0], *where)
+        sra.cache_append(views["k"], views["v"], *caches[1], *where)
+        for a, b in zip(*caches):
+            assert torch.equal(a.view(torch.int16), b.view(torch.int16))
+            assert not torch.equal(a.view(torch.int16), x["k_cache"].view(torch.int16))

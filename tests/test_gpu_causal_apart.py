@@ -1,11 +1,11 @@
-"""What one packed sequence holds does not reach another's outputs or gradients, on the GPU, bitwise."""
+"""What one packed sequence holds does not reach another's outputs or gradients, on the GPU, bitwise; and wide groups of heads."""
 import math
 
 import pytest
 import torch
 
 import paper_2606_13872_amd as sra
-from test_gpu_causal import _inputs
+from test_gpu_causal import _check, _inputs
 
 pytestmark = pytest.mark.gpu
 
@@ -39,3 +39,10 @@ def test_infinities_and_nan_stay_in_their_sequence(nq, nk, heads, kv, d):
                 keep = torch.ones(t.shape[0], dtype=torch.bool, device="cuda")
                 keep[ks if n in ("dk", "dv") else qs] = False
                 assert torch.equal(got[n][keep], t[keep]), (n, b, bad)
+
+
+@pytest.mark.parametrize("heads,kv,d,nq,nk", [(300, 1, 64, [5, 70], [9, 70]), (99, 3, 128, [65, 2], [65, 300])])
+def test_many_heads_of_one_key_head(heads, kv, d, nq, nk):
+    """Items that begin and end inside a token's heads."""
+    print("causal wide groups", heads, kv, d, flush=True)
+    _check(nq, nk, heads, kv, d, seed=17)
