@@ -259,6 +259,8 @@ sra_status sra_launch_export(const sra_problem* p, int which, int32_t* items, in
  *   Errors    as above. Device-resident sizes (sra_tree_attention, sra_cache_append) cannot be refused on the
  *             host: what a call does for bad ones is stated there, and no such value makes it read or write
  *             outside the tensors it was given.
+ *   Roundings sums, maxima, o and the gradients' sums are held in 32 bits; P and dS are rounded to bf16 as inputs of
+ *             the matrix products, and D = rowsum(do o) takes the stored o.
  *   Rows that see no key have o = 0, lse = -inf and no part in any gradient. So have rows whose scores are all
  *             -inf. An infinity or NaN in v (the gradients: in any input) reaches, as in a product with zeros,
  *             also rows and keys of its sequence that the mask keeps apart from it, never another sequence's.
@@ -356,6 +358,8 @@ sra_status sra_tree_workspace_size(const sra_paged_cache* c, int32_t num_heads, 
  * token sees its sequence's whole cached context and, of the sequence's new tokens, those that its mask names, through
  * one softmax (as §4.3 joins cached K/V with the current tokens'). Nothing is written to the cache.
  * q, o: bf16 [tokens, num_heads, head_dim], k, v: the new tokens' bf16 [tokens, num_kv_heads, head_dim].
+ * Lengths may be mixed in any way; the kernel is chosen by the average rows of a sequence (tokens / batch x num_heads /
+ * num_kv_heads, padding included), and long chains are computed with the keys behind each token, masked.
  * tree: device [tokens], bit j of token i's mask = it sees new token j (< 64) of its sequence; itself only if that bit
  *   is set, and later tokens of a longer sequence are seen by none. NULL: a chain of any length, each token sees the
  *   new tokens of its sequence up to itself.

@@ -63,6 +63,8 @@ class CausalPlan:
     """The tile schedule of causal attention for one set of lengths, with its tables on `device` (default: the
     current GPU; without a GPU only the host hooks work). Made once, used by every layer and call with these lengths.
     A plan is made outside a graph's capture, and kept as long as graphs that hold calls with it (they read its tables).
+    Making it, and the first call on another GPU, copies the tables and waits for the current stream: make plans for coming
+    lengths ahead.
 
     q_lens: tokens of each packed sequence. k_lens: its keys, where they differ (the sequence continues earlier
     keys: token i of nq sees the keys j <= i + nk - nq). backward=False plans the forward alone.
@@ -182,8 +184,9 @@ def causal_forward(q, k, v, plan: CausalPlan, scale: Optional[float] = None, out
 
     q: bf16 [tokens, heads, head_dim], k, v: bf16 [keys, kv_heads, head_dim], heads contiguous, a token stride each
     (views of one packed buffer work); query head h reads K/V head h // (heads // kv_heads). o: bf16 like q, dense;
-    lse: fp32 [heads, tokens], natural log. Rows that see no key have o = 0 and lse = -inf. `out` may hold caller
-    buffers o, lse (dense) and workspace (uint8), which must not overlap the inputs. A wrong dtype, shape, layout or
+    lse: fp32 [heads, tokens], natural log. Rows that see no key have o = 0 and lse = -inf. An infinity or NaN in v
+    may reach any row of its sequence. scale: None or <= 0 selects 1 / sqrt(head_dim). `out` may hold caller buffers
+    o, lse (dense) and workspace (uint8), which must not overlap the inputs. A wrong dtype, shape, layout or
     device raises SRAError (SRA_ERR_INVALID_ARGUMENT) before anything reaches the library.
     """
     torch = _s._tm()
@@ -212,7 +215,8 @@ def causal_backward(q, k, v, o, lse, do, plan: CausalPlan, scale: Optional[float
     """Gradients of causal_forward. Returns dict dq, dk, dv (bf16, dense, overwritten).
 
     o and lse as causal_forward wrote them, do: bf16 like o, dense. dk and dv are summed over the query heads that
-    share a K/V head. `out` may hold caller buffers dq, dk, dv (dense) and workspace (uint8).
+    share a K/V head. An infinity or NaN in an input may reach any gradient of its sequence. `out` may hold caller
+    buffers dq, dk, dv (dense) and workspace (uint8).
     """
     torch = _s._tm()
     qs, ks, vs = _qkv(q, k, v, plan)

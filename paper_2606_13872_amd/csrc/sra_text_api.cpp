@@ -162,6 +162,9 @@ sra_status check_cache(const sra_paged_cache* c, bool pointers, bool tensors, Pa
 // More would leave the matrix instructions' columns empty, fewer read K and V once for each of several groups. 16 rows a
 // sequence in groups of 16 take 16.5 us (16 requests of 300 positions), in groups of 32 19.7, shared 19.7; 32 rows in
 // groups of 32 366 us (64 of 8,000), shared 380; 40 rows, 16 of 8,000: 119 us shared.
+// Uneven steps pay for going by the average: 128 single tokens (500 to 8,000 positions) with a chain of 256 tokens over
+// 8,000 take 421 us, by themselves 311 and 61; 64 with a chain of 512 238 us, by themselves 160 and 104. Padding rows count
+// as rows: 64 single tokens 162 us, among 448 padding rows 158 (shared), among 960 172.
 int tree_rows(const sra_paged_cache& c, int32_t heads) {
   const int64_t rows = (int64_t(c.tokens) + c.batch - 1) / c.batch * (heads / c.num_kv_heads);
   return rows <= 16 ? 16 : rows <= 32 ? 32 : kTreeShared;

@@ -19,9 +19,13 @@
 // TB/s of algorithmic bytes, no other bytes fetched; two of 120 to 131 thousand 191 us (5.4 TB/s); four of 31 to 1,500
 // 12 us, a chain of latencies: launch, bounds 1.2 us, first loads 2.5, two chunks 2.5, merge 1, and another 4 us for the
 // second kernel. 64 head dims read 4.4 TB/s (half as long rows); from a cache of a few pages (L2) the kernel takes half
-// the time. Trees of up to 48 tokens over 16 contexts, 40 query heads, both kernels: 82 us, 70 where the last-level
-// cache holds the keys (each 32 rows alone with their keys 226, shared tiles without the software pipeline 125, 32 rows
-// to every wave 80); 64 tokens each over 16 x 16,384 positions 307 us, 890 TFLOP/s.
+// the time. Trees of up to 48 tokens over 16 contexts, 40 query heads, both kernels: 79 us, 77 where the last-level
+// cache holds the keys (before they came to that: each 32 rows alone with their keys 226, shared tiles without the software
+// pipeline 125, 32 rows to every wave 80); 64 tokens each over 16 x 16,384 positions 334 us, 820 TFLOP/s.
+//
+// Chains of many tokens are right but not fast: a group of rows computes all of its sequence's keys, also those behind its
+// last token, and tiles of new tokens run masked, one load and wait after the other. 4,096 tokens over nothing take 448 us
+// (causal attention of packed keys 139), over 8,000 positions 882 (562), 512 tokens 34 (15) and 104 us (79).
 #include "sra_fwd_pipe.h"
 #include "sra_tree.h"
 
@@ -32,8 +36,8 @@ constexpr int kTreeWaves = 4;
 constexpr int kTreeThreads = kTreeWaves * 64;
 constexpr int kSharedChunk = 64;
 // LDS buffers of the shared kernel, for K and for V. Four, with loads two tiles ahead that a tile's end does not wait for:
-// 64 requests of 4,000 positions and 16 tokens, 64 head dims, 134 -> 115 us; groups of more rows 3 % slower, and 128 head
-// dims spill for them.
+// 64 requests of 4,000 positions and 16 tokens, 64 head dims, 134 -> 115 us in turn (112 us on another card, 4.8 TB/s);
+// groups of more rows 3 % slower, and 128 head dims spill for them.
 template <int D, int NQ> constexpr int kTileBufs = D == 64 && NQ == 1 ? 4 : 3;
 constexpr int kNarrow = 128;  // rows of a narrow group of the shared kernel: 16 per wave
 // Costs by C, the keys of a chunk: of beginning a group, of a chunk of a narrow and of a wide group, and of the least run.
